@@ -68,7 +68,11 @@ typedef enum {
     HE_ERR_STATE = 6        /* call order: decode before prefill, prefill on a non-empty cache */
 } he_status;
 
-typedef enum { HE_F32 = 0, HE_BF16 = 1 } he_dtype;
+typedef enum {
+    HE_F32 = 0,
+    HE_BF16 = 1,
+    HE_F16 = 2 /* IEEE binary16: the operators below only; he_create refuses it */
+} he_dtype;
 
 typedef struct {
     int n_layers;      /* L >= 0 */
@@ -271,6 +275,84 @@ he_status he_generate_ragged(he_engine* e, const int32_t* d_prompt_ids, const in
  * 256-row tiles keep every sum whole, so that a sequence scores the same in them and in a batch whose tiles are not cut
  * along k either. */
 he_status he_score(he_engine* e, const int32_t* d_ids, int B, int T, float* d_out_logprobs);
+
+/* ---- Operators of a serving loop over a paged key-value cache
+ *
+ * The engine above reserves max_seq_len positions for every sequence and picks tokens greedily or by Gumbel noise.  A program that
+ * runs the layers itself -- another decoder family, a batch whose sequences come and go -- finds here what it needs next to the
+ * engine's GEMMs: keys and values appended to pages with the rotation of their positions, attention of a prompt and of single tokens,
+ * and a token from a row of logits (the engine's d_logits_opt, or its own).  They need no engine, keep nothing between calls and
+ * allocate nothing; all of a call's work is enqueued on `stream` of the current device and can be captured into a HIP graph.  Calls on
+ * different streams and from different threads may overlap as long as they do not write the same memory.  Arguments are checked on the
+ * host; what device memory holds (lengths, starts, page numbers) is bounds-checked by the kernels as stated.  head_dim is a multiple
+ * of 16 up to 256, a row's head h lies h * head_dim elements behind the row's first, query heads h * n_heads / n_kv_heads and on
+ * share key-value head h, and `data` pointers, rows and pages lie on 16 bytes.  Sums, soft-max statistics and rotations are float;
+ * results are rounded once to dtype. */
+
+/* Text of the last HE_ERR_ an operator gave the calling thread. */
+const char* he_operator_error(void);
+
+/* Row i of a packed batch begins at data + i * stride elements (a view into a wider matrix will do). */
+typedef struct { void* data; int64_t stride; } he_rows;
+
+/* K (V) of position t, key-value head h of sequence b: head_dim elements at
+ *   k + pages[b][t / page_size] * page_stride + (h * page_size + t % page_size) * head_dim.
+ * A sequence has pages_per_seq * page_size positions at most (2^30).  Table entries outside 0 .. n_pages - 1 name no page: nothing is
+ * written through them and their positions count as absent. */
+typedef struct {
+    void *k, *v;          /* DEVICE */
+    const int32_t* pages; /* DEVICE [n_seqs][pages_per_seq] */
+    he_dtype dtype;
+    int n_kv_heads, head_dim;
+    int page_size;        /* positions to a page: a power of two up to 32768 */
+    int n_pages, pages_per_seq;
+    int64_t page_stride;  /* elements from one page to the next, at least n_kv_heads * page_size * head_dim */
+} he_paged_cache;
+
+/* Rotation of pair i of the first `dim` dimensions (a multiple of 16; the others stay) by position * scale * base^(-2 i / dim): pairs
+ * are (x[i], x[i + dim/2]), or (x[2i], x[2i + 1]) with interleaved = 1. */
+typedef struct { int dim; int interleaved; double base; double scale; } he_rope;
+
+/* Appends rows of new tokens.  Sequence b's are rows d_seq_starts[b] .. d_seq_starts[b + 1] - 1 (int32 [n_seqs + 1], ascending; NULL:
+ * row b alone, n_tokens == n_seqs) and go to positions d_lens[b], d_lens[b] + 1, ... (int32 [n_seqs]: positions there already; the
+ * caller adds the new ones).  k is rotated (rope_opt NULL: not) into the cache, and into k_out_opt for attention over the prompt in
+ * flight; v is copied; q_opt [n_tokens, n_heads * head_dim] is rotated into q_out_opt (both or neither).  k_out and q_out may be k and q
+ * themselves.  Rows of no sequence are left out altogether, rows whose position has no page only of the cache. */
+he_status he_paged_append(const he_paged_cache* cache, const he_rope* rope_opt, const he_rows* q_opt, int n_heads, const he_rows* q_out_opt,
+                          const he_rows* k, const he_rows* k_out_opt, const he_rows* v, const int32_t* d_seq_starts_opt, const int32_t* d_lens,
+                          int n_seqs, int n_tokens, void* stream);
+
+/* Attention of one token per sequence over the cache: out[b] = soft-max(scale q[b] . K) V over the positions 0 .. d_lens[b] - 1 of
+ * sequence b (its own among them, so after he_paged_append with the lengths advanced).  A sequence of no positions (d_lens[b] <= 0, or
+ * no page of it exists) gets zeros.  max_len is what the launch is shaped for: about the longest length (0: all that the table can
+ * hold); results are right for any, and the same for the same max_len.  d_workspace: he_paged_attention_workspace bytes with the same
+ * arguments (NULL if that is 0), of any contents, one to every call that may run at the same time. */
+size_t he_paged_attention_workspace(const he_paged_cache* cache, int n_heads, int n_seqs, int max_len);
+he_status he_paged_attention(const he_paged_cache* cache, const he_rows* q, int n_heads, const he_rows* out, const int32_t* d_lens, int n_seqs,
+                             int max_len, float scale, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Attention over whole prompts laid end to end (rows as in he_paged_append): row i of sequence b sees the rows of its sequence up to
+ * itself (causal 1) or all of them (causal 0).  What a row does not see does not reach it, infinities and NaN included.  Rows of no
+ * sequence are left as they were. */
+he_status he_packed_attention(he_dtype dtype, const he_rows* q, int n_heads, const he_rows* k, const he_rows* v, int n_kv_heads, int head_dim,
+                              const he_rows* out, const int32_t* d_seq_starts, int n_seqs, int n_tokens, int causal, float scale, void* stream);
+
+/* A token per row of logits [rows, vocab] (vocab up to 2^20; rows lie on whole elements) from d_uniform [rows], numbers in [0, 1).  With
+ * z the row, T = d_temperature[r] and w[v] = exp((z[v] - max z) / T), tokens in order (larger z first, of equal ones the lower id) are
+ * kept while they are among the first d_top_k[r]; those before them hold less than d_top_p[r] of the first top-k tokens' sum of w; and
+ * w[v] >= d_min_p[r].  The first in order always is.  d_ids[r] is then the first id, in order of ids, at which the running sum of the
+ * kept w exceeds d_uniform[r] times their whole sum (a number of 1 or more: the last kept id), d_logprobs[r] = log_softmax(z)[id] of
+ * the untempered, unfiltered row.  Any of the arrays may be NULL, as filters_opt itself: T = 1, and that filter off; a top_k outside
+ * 1 .. vocab - 1, a top_p of 1 or more and a min_p of 0 or less are off as well; T of 0 or less, or NaN, takes the largest z, of equal
+ * ones the lowest id.  A NaN logit counts as -infinity, which is never drawn; a row of nothing else gets id -1 and log-probability
+ * -infinity.  Sums are taken in 64 bits: the id does not depend on their order. */
+typedef struct {
+    const float* d_temperature; /* [rows] each, or NULL */
+    const int32_t* d_top_k;
+    const float *d_top_p, *d_min_p;
+} he_filters;
+he_status he_sample(he_dtype dtype, const he_rows* logits, int rows, int vocab, const he_filters* filters_opt, const float* d_uniform, int32_t* d_ids,
+                    float* d_logprobs, void* stream);
 
 /* Empties the KV cache (lengths to zero; memory is kept). */
 he_status he_reset(he_engine* e);

@@ -17,7 +17,7 @@ HE_OK = 0
 HE_ERR_INVALID_ARG, HE_ERR_SHAPE, HE_ERR_CAPACITY, HE_ERR_OOM, HE_ERR_DEVICE, HE_ERR_STATE = 1, 2, 3, 4, 5, 6
 STATUS_NAMES = {0: "HE_OK", 1: "HE_ERR_INVALID_ARG", 2: "HE_ERR_SHAPE", 3: "HE_ERR_CAPACITY", 4: "HE_ERR_OOM",
                 5: "HE_ERR_DEVICE", 6: "HE_ERR_STATE"}
-HE_F32, HE_BF16 = 0, 1
+HE_F32, HE_BF16, HE_F16 = 0, 1, 2
 
 
 class he_config(C.Structure):
@@ -60,6 +60,24 @@ class he_sampling(C.Structure):
 class he_pass_plan(C.Structure):
     _fields_ = [("tile_rows", C.c_int), ("tile_cols", C.c_int), ("ksplit", C.c_int), ("split_col", C.c_int),
                 ("scratch_floats", C.c_size_t), ("scratch_reserved", C.c_size_t), ("workgroup_cols", C.c_int)]
+
+
+class he_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64)]
+
+
+class he_paged_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_void_p), ("dtype", C.c_int), ("n_kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("page_size", C.c_int), ("n_pages", C.c_int), ("pages_per_seq", C.c_int),
+                ("page_stride", C.c_int64)]
+
+
+class he_rope(C.Structure):
+    _fields_ = [("dim", C.c_int), ("interleaved", C.c_int), ("base", C.c_double), ("scale", C.c_double)]
+
+
+class he_filters(C.Structure):
+    _fields_ = [("d_temperature", C.c_void_p), ("d_top_k", C.c_void_p), ("d_top_p", C.c_void_p), ("d_min_p", C.c_void_p)]
 
 
 class HeError(RuntimeError):
@@ -157,6 +175,19 @@ def lib() -> C.CDLL:
     L.he_calibration_copy.argtypes = [vp, vp, C.c_size_t, vp]
     L.he_rng_words.restype = C.c_int
     L.he_rng_words.argtypes = [C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32, C.c_int, vp, vp]
+    rows = C.POINTER(he_rows)
+    L.he_operator_error.restype = C.c_char_p
+    L.he_operator_error.argtypes = []
+    L.he_paged_append.restype = C.c_int
+    L.he_paged_append.argtypes = [C.POINTER(he_paged_cache), C.POINTER(he_rope), rows, C.c_int, rows, rows, rows, rows, ip, ip, C.c_int, C.c_int, vp]
+    L.he_paged_attention_workspace.restype = C.c_size_t
+    L.he_paged_attention_workspace.argtypes = [C.POINTER(he_paged_cache), C.c_int, C.c_int, C.c_int]
+    L.he_paged_attention.restype = C.c_int
+    L.he_paged_attention.argtypes = [C.POINTER(he_paged_cache), rows, C.c_int, rows, ip, C.c_int, C.c_int, C.c_float, vp, C.c_size_t, vp]
+    L.he_packed_attention.restype = C.c_int
+    L.he_packed_attention.argtypes = [C.c_int, rows, C.c_int, rows, rows, C.c_int, C.c_int, rows, ip, C.c_int, C.c_int, C.c_int, C.c_float, vp]
+    L.he_sample.restype = C.c_int
+    L.he_sample.argtypes = [C.c_int, rows, C.c_int, C.c_int, C.POINTER(he_filters), fp, ip, fp, vp]
     _lib = L
     return L
 
@@ -169,7 +200,8 @@ EXPORTS = ("he_workspace_bytes", "he_create", "he_refresh_weights", "he_prefill"
            "he_tile_matrix_lora", "he_plan_decode_gemm", "he_fp8_quantize_rows", "he_decode_step_static",
            "he_decode_scratch_account", "he_arrival_counters_nonzero", "he_arrival_counters_set", "he_last_step_rows",
            "he_plan_prompt_gemm", "he_plan_pass_gemm", "he_plan_attention", "he_plan_plain_gemm", "he_plan_weight_copies",
-           "he_plan_fetch_ahead")
+           "he_plan_fetch_ahead", "he_operator_error", "he_paged_append", "he_paged_attention_workspace", "he_paged_attention",
+           "he_packed_attention", "he_sample")
 
 KERNEL_CLASSES = ("layernorm", "qkv", "attention", "out_proj", "fc1", "fc2", "lm_head", "empty")
 
@@ -530,3 +562,167 @@ def tile_weights_in_place(weights: dict) -> dict:
     out["lm_head"] = he_tile_matrix(weights["lm_head"])
     torch.cuda.synchronize()
     return out
+
+
+# ---- operators of a serving loop (he.h): torch tensors in, one call each, on the current stream of the tensors' device
+
+_OPERATOR_DTYPES = None
+
+
+def _need(ok, text):
+    if not ok:
+        raise HeError(HE_ERR_INVALID_ARG, text)
+
+
+def _dtype(t):
+    global _OPERATOR_DTYPES
+    if _OPERATOR_DTYPES is None:
+        import torch
+        _OPERATOR_DTYPES = {torch.float32: HE_F32, torch.bfloat16: HE_BF16, torch.float16: HE_F16}
+    code = _OPERATOR_DTYPES.get(t.dtype)
+    _need(code is not None, f"tensors are float32, bfloat16 or float16, not {t.dtype}")
+    return code
+
+
+def _call(tensor, entry, *args):
+    """entry(*args, the current stream of the tensor's device), with that device current."""
+    import torch
+    if tensor.device.index != torch.cuda.current_device():
+        with torch.cuda.device(tensor.device):
+            rc = entry(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        rc = entry(*args, torch.cuda.current_stream().cuda_stream)
+    if rc != HE_OK:
+        raise HeError(rc, (lib().he_operator_error() or b"").decode())
+
+
+def _on(first, *others):
+    _need(first.is_cuda, "tensors live on the GPU")
+    for t in others:
+        _need(t is None or t.device == first.device, "all tensors live on one device")
+
+
+def _token_rows(t, like, heads, dim, name):
+    """A [rows, heads, dim] view whose rows may lie apart, as he_rows."""
+    _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim and t.dtype == like.dtype, f"{name} is [rows, {heads}, {dim}] of {like.dtype}")
+    _need((t.stride(2) == 1 or dim == 1) and (t.stride(1) == dim or heads == 1), f"{name}: heads of a row lie side by side")
+    return he_rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim)
+
+
+def _ints(t, shape, name):
+    import torch
+    _need(t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous(), f"{name} is a contiguous int32 tensor of shape {list(shape)}")
+    return t.data_ptr()
+
+
+def _floats(t, n, name):
+    import torch
+    if t is None:
+        return None
+    _need(t.dtype == torch.float32 and tuple(t.shape) == (n,) and t.is_contiguous(), f"{name} is a contiguous float32 tensor of {n}")
+    return t.data_ptr()
+
+
+def _cache(k_pages, v_pages, pages):
+    _need(k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype, "K and V pages are [n_pages, kv heads, page_size, dim]")
+    n, heads, size, dim = k_pages.shape
+    for t in (k_pages, v_pages):
+        _need(t.stride(3) == 1 and t.stride(2) == dim and (t.stride(1) == size * dim or heads == 1), "a page is contiguous")
+    _need(k_pages.stride(0) == v_pages.stride(0) or n == 1, "K and V pages lie equally far apart")
+    _need(pages.dim() == 2, "the page table is [sequences, pages_per_seq]")
+    return he_paged_cache(k_pages.data_ptr(), v_pages.data_ptr(), _ints(pages, tuple(pages.shape), "the page table"), _dtype(k_pages), heads, dim, size, n,
+                          pages.shape[1], k_pages.stride(0) if n > 1 else heads * size * dim)
+
+
+def rope(dim: int, base: float = 10000.0, scale: float = 1.0, interleaved: bool = False) -> he_rope:
+    return he_rope(dim, 1 if interleaved else 0, base, scale)
+
+
+def he_paged_append(k, v, k_pages, v_pages, pages, lens, seq_starts=None, q=None, q_out=None, k_out=None, rope=None):
+    """Appends rows k, v [n, kv heads, dim] to the pages [n_pages, kv heads, page_size, dim] of their sequences, keys rotated by `rope`; queries q
+    [n, heads, dim] are rotated into q_out (which may be q), keys into k_out if that is given."""
+    _on(k, v, k_pages, v_pages, pages, lens, seq_starts, q, q_out, k_out)
+    c = _cache(k_pages, v_pages, pages)
+    n, seqs, h, d = k.shape[0], pages.shape[0], c.n_kv_heads, c.head_dim
+    _need(v.shape == k.shape and (q is None) == (q_out is None), "k and v have as many rows; q comes with q_out")
+    qr = qo = ko = None
+    heads = 0
+    if n == 0:  # (an empty tensor has no address to name)
+        return
+    if q is not None:
+        _need(q.dim() == 3 and q.shape[0] == n and q_out.shape == q.shape, "q and q_out have as many rows as k")
+        heads = q.shape[1]
+        qr, qo = _token_rows(q, k_pages, heads, d, "q"), _token_rows(q_out, k_pages, heads, d, "q_out")
+    if k_out is not None:
+        _need(k_out.shape == k.shape, "k_out has as many rows as k")
+        ko = _token_rows(k_out, k_pages, h, d, "k_out")
+    _call(k, lib().he_paged_append, c, rope, qr, heads, qo, _token_rows(k, k_pages, h, d, "k"), ko, _token_rows(v, k_pages, h, d, "v"),
+          None if seq_starts is None else _ints(seq_starts, (seqs + 1,), "seq_starts"), _ints(lens, (seqs,), "lens"), seqs, n)
+
+
+def he_paged_attention_workspace(k_pages, v_pages, pages, heads: int, max_len: int = 0) -> int:
+    """Bytes of workspace that he_paged_attention needs for as many sequences as the page table has."""
+    return lib().he_paged_attention_workspace(_cache(k_pages, v_pages, pages), heads, pages.shape[0], max_len)
+
+
+def he_paged_attention(q, k_pages, v_pages, pages, lens, max_len: int = 0, scale: Optional[float] = None, out=None, workspace=None):
+    """One token per sequence, q [sequences, heads, dim], over the first lens[b] positions of its pages; scale: dim^-0.5 unless given.  workspace: a
+    tensor of he_paged_attention_workspace bytes for a program that keeps one."""
+    import torch
+    _on(q, k_pages, v_pages, pages, lens, out, workspace)
+    c = _cache(k_pages, v_pages, pages)
+    seqs, d = pages.shape[0], c.head_dim
+    _need(q.dim() == 3 and q.shape[0] == seqs, "q is [sequences, heads, dim]")
+    heads = q.shape[1]
+    if out is None:
+        out = torch.empty(seqs, heads, d, dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape, "out has the shape of q")
+    if seqs == 0:
+        return out
+    nbytes = lib().he_paged_attention_workspace(c, heads, seqs, max_len)
+    if workspace is None and nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    have = 0
+    if workspace is not None:
+        _need(workspace.is_contiguous(), "workspace is contiguous")
+        have = workspace.numel() * workspace.element_size()
+    _call(q, lib().he_paged_attention, c, _token_rows(q, k_pages, heads, d, "q"), heads, _token_rows(out, k_pages, heads, d, "out"), _ints(lens, (seqs,), "lens"),
+          seqs, max_len, d ** -0.5 if scale is None else scale, _ptr(workspace), have)
+    return out
+
+
+def he_packed_attention(q, k, v, seq_starts, causal: bool = True, scale: Optional[float] = None, out=None):
+    """Prompts laid end to end: q [n, heads, dim], k and v [n, kv heads, dim], sequence b in rows seq_starts[b] .. seq_starts[b + 1] - 1."""
+    import torch
+    _on(q, k, v, seq_starts, out)
+    _need(q.dim() == 3 and k.dim() == 3 and v.shape == k.shape and k.shape[0] == q.shape[0], "q is [n, heads, dim], k and v [n, kv heads, dim]")
+    n, heads, d = q.shape
+    if out is None:
+        out = torch.empty(n, heads, d, dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape, "out has the shape of q")
+    _need(seq_starts.dim() == 1 and seq_starts.shape[0] >= 1, "seq_starts is [sequences + 1]")
+    seqs, hk = seq_starts.shape[0] - 1, k.shape[1]
+    if n == 0:
+        return out
+    _call(q, lib().he_packed_attention, _dtype(q), _token_rows(q, q, heads, d, "q"), heads, _token_rows(k, q, hk, d, "k"), _token_rows(v, q, hk, d, "v"), hk, d,
+          _token_rows(out, q, heads, d, "out"), _ints(seq_starts, (seqs + 1,), "seq_starts"), seqs, n, 1 if causal else 0, d ** -0.5 if scale is None else scale)
+    return out
+
+
+def he_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
+    """(ids int32 [rows], log-probabilities float32 [rows]) of a token per row of logits [rows, vocab], from the numbers uniform [rows] in [0, 1);
+    the filters are tensors of a value per row, or None."""
+    import torch
+    _on(logits, uniform, temperature, top_k, top_p, min_p)
+    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits are [rows, vocab], a row contiguous")
+    rows, vocab = logits.shape
+    ids = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    logprobs = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    if rows == 0:
+        return ids, logprobs
+    _need(uniform is not None, "uniform is needed")
+    f = he_filters(_floats(temperature, rows, "temperature"), None if top_k is None else _ints(top_k, (rows,), "top_k"), _floats(top_p, rows, "top_p"),
+                   _floats(min_p, rows, "min_p"))
+    _call(logits, lib().he_sample, _dtype(logits), he_rows(logits.data_ptr(), logits.stride(0)), rows, vocab, f, _floats(uniform, rows, "uniform"),
+          ids.data_ptr(), logprobs.data_ptr())
+    return ids, logprobs
