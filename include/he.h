@@ -292,7 +292,7 @@ he_status he_score(he_engine* e, const int32_t* d_ids, int B, int T, float* d_ou
 /* Text of the last HE_ERR_ an operator gave the calling thread. */
 const char* he_operator_error(void);
 
-/* Row i of a packed batch begins at data + i * stride elements (a view into a wider matrix will do). */
+/* Row i of a packed batch begins at data + i * stride elements (a view into a wider matrix will do; 2^22 at most). */
 typedef struct { void* data; int64_t stride; } he_rows;
 
 /* K (V) of position t, key-value head h of sequence b: head_dim elements at
@@ -337,7 +337,7 @@ he_status he_paged_attention(const he_paged_cache* cache, const he_rows* q, int 
 he_status he_packed_attention(he_dtype dtype, const he_rows* q, int n_heads, const he_rows* k, const he_rows* v, int n_kv_heads, int head_dim,
                               const he_rows* out, const int32_t* d_seq_starts, int n_seqs, int n_tokens, int causal, float scale, void* stream);
 
-/* A token per row of logits [rows, vocab] (vocab up to 2^20; rows lie on whole elements) from d_uniform [rows], numbers in [0, 1).  With
+/* A token per row of logits [rows, vocab] (vocab up to 2^20; rows lie on whole elements, any distance apart) from d_uniform [rows], numbers in [0, 1).  With
  * z the row, T = d_temperature[r] and w[v] = exp((z[v] - max z) / T), tokens in order (larger z first, of equal ones the lower id) are
  * kept while they are among the first d_top_k[r]; those before them hold less than d_top_p[r] of the first top-k tokens' sum of w; and
  * w[v] >= d_min_p[r].  The first in order always is.  d_ids[r] is then the first id, in order of ids, at which the running sum of the

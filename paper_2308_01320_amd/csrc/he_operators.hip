@@ -38,6 +38,7 @@ he_status check_rows(const he_rows* r, const char* name, he_dtype t, int64_t wid
     if (!r || !r->data) return refuse(HE_ERR_INVALID_ARG, "%s is NULL", name);
     if (!aligned(r->data)) return refuse(HE_ERR_SHAPE, "%s does not lie on 16 bytes", name);
     if (r->stride < 0 || r->stride * elt_bytes(t) % 16) return refuse(HE_ERR_SHAPE, "%s: rows %lld elements apart: a multiple of 16 bytes", name, (long long)r->stride);
+    if (r->stride > 1 << 22) return refuse(HE_ERR_SHAPE, "%s: rows %lld elements apart: 2^22 at most", name, (long long)r->stride);
     if (out && r->stride < width)
         return refuse(HE_ERR_SHAPE, "%s: rows %lld elements apart, each has %lld", name, (long long)r->stride, (long long)width);
     return HE_OK;
