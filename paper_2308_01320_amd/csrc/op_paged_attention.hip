@@ -63,6 +63,233 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(Cache c, Rows q, i
     attend<E, DP, GQ>(sh, begin, end, d, qs, rows, emit);
 }
 
+// The same on the matrix cores, for the 16-bit types and pages of 16 positions or more: up to sixteen queries that share their keys are the columns
+// of S^T = K Q^T and O^T = V^T P^T.  A wavefront has every fourth tile of 32 keys to itself, from the loads to its own part of the result,
+// so nothing in the loop waits for another: K goes from memory into operands, V past the registers into LDS, both a tile ahead, and V is
+// transposed by the reads.  A lane holds one query; its four keys of each half of the tile are four of its weights' eight places, in the
+// order in which V's rows are read.  Weights multiply V as two terms of the type, so that nothing of them is lost that float has.
+template <class E, int DP, bool EXACT>
+struct PagedTile {
+    static constexpr int CPR = DP / 8, LOADS = DP / 16, RPN = 64 / CPR;  // 16-byte pieces of a row; copies of V per tile, rows of each
+    static __device__ __forceinline__ int turn(int r) { return CPR >= 16 ? (r & 7) << 1 : r & 6; }  // (as in the prompts' tiles)
+};
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4 mma16(BF16, const u32x4& a, const u32x4& b, f32x4 c) {
+    typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(F16, const u32x4& a, const u32x4& b, f32x4 c) {
+    typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+}
+
+// Four operands of V^T: blocks of sixteen dimensions at the four places, keys 4 g + 0..3 and 16 + 4 g + 0..3 (g = lane / 16), BYTES apart
+template <int BYTES>
+__device__ __forceinline__ void v_operands(u32x4 (&o)[4], const uint32_t (&at)[4]) {
+    uint2 r[8];
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(BYTES)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = u32x4{r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y};
+}
+
+template <class E, int DP, bool EXACT>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_mma_kernel(Cache c, Rows q, int n_heads, Rows out, const int32_t* __restrict__ lens, int splits, float scale,
+                                                                           float* __restrict__ workspace) {
+    typedef typename E::T T;
+    typedef PagedTile<E, DP, EXACT> Ti;
+    constexpr int KB = DP / 32, OB = DP / 16, PITCH = DP + 4, REGION = 2 * 32 * DP * 2;  // a wavefront's two tiles of V, in bytes
+    extern __shared__ __align__(1024) unsigned char smem[];
+    __shared__ float2 ml[4][16];
+    const int d = EXACT ? DP : c.head_dim, share = n_heads / c.n_kv_heads, groups = (share + 15) / 16;
+    const int part = blockIdx.x % splits, rest = blockIdx.x / splits, h = rest / groups, g0 = rest % groups * 16, b = blockIdx.y, nq = min(16, share - g0);
+    const int len = (int)min((int64_t)max(lens[b], 0), (int64_t)c.pages_per_seq << c.page_shift);
+    int begin, end;
+    share_of(len, splits, part, begin, end);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+    const int n_tiles = (end - begin + 31) / 32;
+    const int32_t* table = c.pages + (size_t)b * c.pages_per_seq;
+    // the pages of the two halves of a tile, -1: none
+    struct Pages { int p[2]; };
+    auto pages = [&](int tile) {
+        Pages r;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int t = begin + tile * 32 + x * 16;
+            const int p = t < end ? table[t >> c.page_shift] : -1;
+            r.p[x] = (unsigned)p < (unsigned)c.n_pages ? p : -1;
+        }
+        return r;
+    };
+    auto offset = [&](const Pages& pg, int tile, int x) {  // of the first row of half x, in elements; of a page that is none: page 0's
+        return cache_row(c, max(pg.p[x], 0), h, begin + tile * 32 + x * 16);
+    };
+    unsigned char* region = smem + wave * REGION;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)region;
+    uint32_t v_place[Ti::LOADS];  // a lane's row and piece of each copy
+#pragma unroll
+    for (int n = 0; n < Ti::LOADS; ++n) {
+        const int r = n * Ti::RPN + lane / Ti::CPR;
+        int pc = (lane % Ti::CPR) ^ Ti::turn(r);
+        if (!EXACT) pc = min(pc, d / 8 - 1);
+        v_place[n] = (r & 15) * d + pc * 8;
+    }
+    auto request_v = [&](const Pages& pg, int tile, int buf) {
+        const T* at[2] = {(const T*)c.v + offset(pg, tile, 0), (const T*)c.v + offset(pg, tile, 1)};
+#pragma unroll
+        for (int n = 0; n < Ti::LOADS; ++n)
+            he_bf16::load_block_to_lds<true>(reinterpret_cast<const u32x4*>(at[n * Ti::RPN / 16] + v_place[n]), reinterpret_cast<u32x4*>(region + buf * (REGION / 2)) + n * 64);
+    };
+    auto request_k = [&](const Pages& pg, int tile, u32x4 (&k)[2][KB]) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const T* at = (const T*)c.k + offset(pg, tile, x) + j * d + g * 8;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                k[x][kb] = u32x4{0u, 0u, 0u, 0u};
+                if (EXACT || kb * 32 + g * 8 < d) k[x][kb] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at + kb * 32));
+            }
+        }
+    };
+    u32x4 k[2][KB], qo[KB];
+    Pages now = pages(wave), next = pages(wave + 4);
+    if (wave < n_tiles) {
+        request_v(now, wave, 0);
+        asm volatile("" ::: "memory");  // K behind V: loads come back in order, so whoever has K has V in LDS
+        request_k(now, wave, k);
+    }
+    {
+        const T* qp = (const T*)q.data + (int64_t)b * q.stride + (int64_t)(h * share + g0 + min(j, nq - 1)) * d + g * 8;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) qo[kb] = EXACT || kb * 32 + g * 8 < d ? *reinterpret_cast<const u32x4*>(qp + kb * 32) : u32x4{0u, 0u, 0u, 0u};
+    }
+    const float cs = scale * 1.44269504f;
+    f32x4 o[OB];
+#pragma unroll
+    for (int i = 0; i < OB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    uint32_t read_at[OB];
+#pragma unroll
+    for (int i = 0; i < OB; ++i) {
+        const int row = 4 * g + (j >> 2), pc = i * 2 + ((j & 3) >> 1);
+        read_at[i] = lds0 + (row * Ti::CPR + (pc ^ Ti::turn(row))) * 16 + (j & 1) * 8;
+    }
+    float m = -INFINITY, l = 0.f;
+    int buf = 0;
+    for (int tile = wave; tile < n_tiles; tile += 4) {
+        f32x4 s[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            s[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                if (EXACT || kb * 32 < d) s[x] = mma16(E{}, k[x][kb], qo[kb], s[x]);
+        }
+        asm volatile("" : "+v"(s[0]), "+v"(s[1])::"memory");  // (K has been waited for, and with it V)
+        const Pages after = pages(tile + 8);
+        if (tile + 4 < n_tiles) {
+            request_v(next, tile + 4, buf ^ 1);  // (its reads were over when the tile before this one was)
+            asm volatile("" ::: "memory");
+            request_k(next, tile + 4, k);
+        }
+        const int t0 = begin + tile * 32;
+        const int n0 = now.p[0] < 0 ? 0 : min(end - t0, 16), n1 = now.p[1] < 0 ? 0 : min(end - t0 - 16, 16);  // keys of each half
+        s[0] *= cs;
+        s[1] *= cs;
+        if (n0 < 16 || n1 < 16) {
+            // rows that do not count may hold anything: no weight, and zeros for it to multiply
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (4 * g + r >= n0) s[0][r] = -INFINITY;
+                if (4 * g + r >= n1) s[1][r] = -INFINITY;
+            }
+#pragma unroll
+            for (int n = 0; n < Ti::LOADS; ++n) {
+                const int r = n * Ti::RPN + lane / Ti::CPR;
+                if ((r & 15) >= (r < 16 ? n0 : n1)) reinterpret_cast<u32x4*>(region + buf * (REGION / 2))[n * 64 + lane] = u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) top = fmaxf(top, s[r >> 2][r & 3]);
+        top = fmaxf(m, lane_max32_apart(lane_max16_apart(top)));
+        const float ref = top > -INFINITY ? top : 0.f;
+        if (__any(top > m)) {
+            const float keep = __builtin_amdgcn_exp2f(m - ref);
+            l *= keep;
+#pragma unroll
+            for (int i = 0; i < OB; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[i][r] *= keep;
+            m = top;
+        }
+        float w[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) w[r] = __builtin_amdgcn_exp2f(s[r >> 2][r & 3] - ref);
+        l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            hi[r] = E::pack(w[2 * r], w[2 * r + 1]);
+            lo[r] = E::pack(w[2 * r] - E::lo(hi[r]), w[2 * r + 1] - E::hi(hi[r]));
+        }
+        const u32x4 wh = {hi[0], hi[1], hi[2], hi[3]}, wl = {lo[0], lo[1], lo[2], lo[3]};
+#pragma unroll
+        for (int i = 0; i < OB; i += 4) {
+            if (!EXACT && i * 16 >= d) continue;
+            uint32_t at[4];
+            u32x4 v[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) at[x] = read_at[i + x] + buf * (REGION / 2);
+            v_operands<16 * Ti::CPR * 16>(v, at);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                o[i + x] = mma16(E{}, v[x], wl, o[i + x]);
+                o[i + x] = mma16(E{}, v[x], wh, o[i + x]);
+            }
+        }
+        now = next;
+        next = after;
+        buf ^= 1;
+    }
+    l = lane_sum32_apart(lane_sum16_apart(l));
+    float* mine = reinterpret_cast<float*>(region);
+#pragma unroll
+    for (int i = 0; i < OB; ++i)
+        if (j < nq) *reinterpret_cast<f32x4*>(mine + j * PITCH + i * 16 + 4 * g) = o[i];
+    if (g == 0) ml[wave][j] = make_float2(m, l);
+    __syncthreads();
+    const Partial part_at = partial_of(workspace, (size_t)gridDim.y * n_heads, splits);
+    for (int x = threadIdx.x; x < nq * (d / 2); x += 256) {
+        const int qi = x / (d / 2), e = x % (d / 2) * 2, head = h * share + g0 + qi;
+        float top = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][qi].x);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 a = ml[w][qi], v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(smem + w * REGION) + qi * PITCH + e);
+            const float f = a.x > -INFINITY ? __builtin_amdgcn_exp2f(a.x - top) : a.y;
+            sum += a.y * f;
+            o0 += v.x * f;
+            o1 += v.y * f;
+        }
+        if (splits == 1) {
+            *reinterpret_cast<uint32_t*>((T*)out.data + (int64_t)b * out.stride + (int64_t)head * d + e) = E::pack(attended(sum, o0), attended(sum, o1));
+            continue;
+        }
+        const size_t row = ((size_t)b * n_heads + head) * splits + part;
+        if (e == 0) part_at.ml[row] = make_float2(top * 0.693147181f, sum);  // (the join's maxima are natural)
+        *reinterpret_cast<float2*>(part_at.o + row * d + e) = make_float2(o0, o1);
+    }
+}
+
 // The splits of a row, weighted by exp(their maximum - the largest)
 template <class E>
 __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ workspace, Rows out, int n_heads, int d, int splits) {
@@ -99,6 +326,21 @@ void paged_attention(hipStream_t s, he_dtype dt, const Cache& c, Rows q, int n_h
     const int share = n_heads / c.n_kv_heads;
     by_type(dt, [&](auto e) {
         typedef decltype(e) E;
+        if constexpr (sizeof(typename E::T) == 2) {
+            if (c.page_shift >= 4) {  // (a half of a tile lies in one page)
+                auto launch = [&](auto dp, auto exact) {
+                    constexpr int DP = decltype(dp)::value;
+                    paged_mma_kernel<E, DP, decltype(exact)::value>
+                        <<<dim3(c.n_kv_heads * ((share + 15) / 16) * splits, n_seqs), 256, 4 * 2 * 32 * DP * 2, s>>>(c, q, n_heads, out, lens, splits, scale, workspace);
+                };
+                if (c.head_dim == 64) launch(std::integral_constant<int, 64>{}, std::true_type{});
+                else if (c.head_dim == 128) launch(std::integral_constant<int, 128>{}, std::true_type{});
+                else if (c.head_dim < 128) launch(std::integral_constant<int, 128>{}, std::false_type{});
+                else launch(std::integral_constant<int, 256>{}, std::false_type{});
+                if (splits > 1) join_kernel<E><<<n_seqs * n_heads, 256, 0, s>>>(workspace, out, n_heads, c.head_dim, splits);
+                return;
+            }
+        }
         auto launch = [&](auto dp, auto gq) {
             constexpr int DP = decltype(dp)::value, GQ = decltype(gq)::value;
             const int groups = (share + GQ - 1) / GQ;
