@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -565,73 +566,104 @@ def tile_weights_in_place(weights: dict) -> dict:
 
 
 # ---- operators of a serving loop (he.h): torch tensors in, one call each, on the current stream of the tensors' device
+#
+# A step of a serving loop makes these calls by the hundred, and the smallest of their kernels take 4 us: arguments are looked at once each, the
+# structures of he.h are packed as bytes, and messages are put together only for a refusal.
 
-_OPERATOR_DTYPES = None
+_ROWS = struct.Struct("@Pq").pack          # he_rows
+_CACHE = struct.Struct("@PPPiiiiiiq").pack  # he_paged_cache
+_FILTERS = struct.Struct("@PPPP").pack      # he_filters
+_ops = None
 
 
-def _need(ok, text):
-    if not ok:
-        raise HeError(HE_ERR_INVALID_ARG, text)
+class _Operators:
+    """The library's entries with byte strings for structures, and what of torch the calls need."""
 
-
-def _dtype(t):
-    global _OPERATOR_DTYPES
-    if _OPERATOR_DTYPES is None:
+    def __init__(self):
         import torch
-        _OPERATOR_DTYPES = {torch.float32: HE_F32, torch.bfloat16: HE_BF16, torch.float16: HE_F16}
-    code = _OPERATOR_DTYPES.get(t.dtype)
-    _need(code is not None, f"tensors are float32, bfloat16 or float16, not {t.dtype}")
+        L, p, i = lib(), C.c_void_p, C.c_int
+        self.torch, self.codes = torch, {torch.float32: HE_F32, torch.bfloat16: HE_BF16, torch.float16: HE_F16}
+        self.device, self.stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+        def entry(name, *types, restype=C.c_int):
+            f = L[name]  # (an object of its own, beside the one that lib() declares)
+            f.argtypes, f.restype = types, restype
+            return f
+
+        self.append = entry("he_paged_append", p, p, p, i, p, p, p, p, p, p, i, i, p)
+        self.workspace = entry("he_paged_attention_workspace", p, i, i, i, restype=C.c_size_t)
+        self.paged = entry("he_paged_attention", p, p, i, p, p, i, i, C.c_float, p, C.c_size_t, p)
+        self.packed = entry("he_packed_attention", i, p, i, p, p, i, i, p, p, i, i, i, C.c_float, p)
+        self.sample = entry("he_sample", i, p, i, i, p, p, p, p, p)
+
+    def call(self, dev, entry, *args):
+        if self.device() != dev:
+            with self.torch.cuda.device(dev):
+                rc = entry(*args, self.stream(dev))
+        else:
+            rc = entry(*args, self.stream(dev))
+        if rc != HE_OK:
+            raise HeError(rc, (lib().he_operator_error() or b"").decode())
+
+
+def _operators() -> _Operators:
+    global _ops
+    if _ops is None:
+        _ops = _Operators()
+    return _ops
+
+
+def _bad(text):
+    raise HeError(HE_ERR_INVALID_ARG, text)
+
+
+def _device(t):
+    dev = t.get_device()
+    if dev < 0:
+        _bad("tensors live on the GPU")
+    return dev
+
+
+def _code(ops, t):
+    code = ops.codes.get(t.dtype)
+    if code is None:
+        _bad(f"tensors are float32, bfloat16 or float16, not {t.dtype}")
     return code
 
 
-def _call(tensor, entry, *args):
-    """entry(*args, the current stream of the tensor's device), with that device current."""
-    import torch
-    if tensor.device.index != torch.cuda.current_device():
-        with torch.cuda.device(tensor.device):
-            rc = entry(*args, torch.cuda.current_stream().cuda_stream)
-    else:
-        rc = entry(*args, torch.cuda.current_stream().cuda_stream)
-    if rc != HE_OK:
-        raise HeError(rc, (lib().he_operator_error() or b"").decode())
+def _token_rows(t, dev, dtype, n, heads, dim, name):
+    """A [n, heads, dim] view whose rows may lie apart, as he_rows."""
+    if t.shape != (n, heads, dim) or t.dtype != dtype or t.get_device() != dev:
+        _bad(f"{name} is [{n}, {heads}, {dim}] of {dtype} on device {dev}")
+    apart, head, one = t.stride()
+    if one != 1 or (head != dim and heads != 1):
+        _bad(f"{name}: heads of a row lie side by side")
+    return _ROWS(t.data_ptr(), apart if n > 1 else heads * dim)
 
 
-def _on(first, *others):
-    _need(first.is_cuda, "tensors live on the GPU")
-    for t in others:
-        _need(t is None or t.device == first.device, "all tensors live on one device")
-
-
-def _token_rows(t, like, heads, dim, name):
-    """A [rows, heads, dim] view whose rows may lie apart, as he_rows."""
-    _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim and t.dtype == like.dtype, f"{name} is [rows, {heads}, {dim}] of {like.dtype}")
-    _need((t.stride(2) == 1 or dim == 1) and (t.stride(1) == dim or heads == 1), f"{name}: heads of a row lie side by side")
-    return he_rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim)
-
-
-def _ints(t, shape, name):
-    import torch
-    _need(t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous(), f"{name} is a contiguous int32 tensor of shape {list(shape)}")
+def _plain(ops, t, dev, dtype, n, name):
+    """Address of a contiguous vector of n."""
+    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.get_device() != dev:
+        _bad(f"{name} is a contiguous {dtype} tensor of {n} on device {dev}")
     return t.data_ptr()
 
 
-def _floats(t, n, name):
-    import torch
-    if t is None:
-        return None
-    _need(t.dtype == torch.float32 and tuple(t.shape) == (n,) and t.is_contiguous(), f"{name} is a contiguous float32 tensor of {n}")
-    return t.data_ptr()
-
-
-def _cache(k_pages, v_pages, pages):
-    _need(k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype, "K and V pages are [n_pages, kv heads, page_size, dim]")
-    n, heads, size, dim = k_pages.shape
-    for t in (k_pages, v_pages):
-        _need(t.stride(3) == 1 and t.stride(2) == dim and (t.stride(1) == size * dim or heads == 1), "a page is contiguous")
-    _need(k_pages.stride(0) == v_pages.stride(0) or n == 1, "K and V pages lie equally far apart")
-    _need(pages.dim() == 2, "the page table is [sequences, pages_per_seq]")
-    return he_paged_cache(k_pages.data_ptr(), v_pages.data_ptr(), _ints(pages, tuple(pages.shape), "the page table"), _dtype(k_pages), heads, dim, size, n,
-                          pages.shape[1], k_pages.stride(0) if n > 1 else heads * size * dim)
+def _cache(ops, k_pages, v_pages, pages, dev):
+    """he_paged_cache, and [sequences, kv heads, head_dim] of it."""
+    shape, at = k_pages.shape, k_pages.stride()
+    if len(shape) != 4 or v_pages.shape != shape or v_pages.dtype != k_pages.dtype or k_pages.get_device() != dev or v_pages.get_device() != dev:
+        _bad(f"K and V pages are [n_pages, kv heads, page_size, dim] of one type on device {dev}")
+    n, heads, size, dim = shape
+    if v_pages.stride() != at and n > 1:
+        _bad("K and V pages are laid out alike")
+    for s in (at, v_pages.stride()):
+        if s[3] != 1 or (s[2] != dim and size != 1) or (s[1] != size * dim and heads != 1):
+            _bad("a page is contiguous")
+    if pages.dtype != ops.torch.int32 or pages.dim() != 2 or not pages.is_contiguous() or pages.get_device() != dev:
+        _bad(f"the page table is a contiguous int32 tensor [sequences, pages_per_seq] on device {dev}")
+    seqs, per_seq = pages.shape
+    return _CACHE(k_pages.data_ptr(), v_pages.data_ptr(), pages.data_ptr(), _code(ops, k_pages), heads, dim, size, n, per_seq,
+                  at[0] if n > 1 else heads * size * dim), seqs, heads, dim
 
 
 def rope(dim: int, base: float = 10000.0, scale: float = 1.0, interleaved: bool = False) -> he_rope:
@@ -641,88 +673,97 @@ def rope(dim: int, base: float = 10000.0, scale: float = 1.0, interleaved: bool 
 def he_paged_append(k, v, k_pages, v_pages, pages, lens, seq_starts=None, q=None, q_out=None, k_out=None, rope=None):
     """Appends rows k, v [n, kv heads, dim] to the pages [n_pages, kv heads, page_size, dim] of their sequences, keys rotated by `rope`; queries q
     [n, heads, dim] are rotated into q_out (which may be q), keys into k_out if that is given."""
-    _on(k, v, k_pages, v_pages, pages, lens, seq_starts, q, q_out, k_out)
-    c = _cache(k_pages, v_pages, pages)
-    n, seqs, h, d = k.shape[0], pages.shape[0], c.n_kv_heads, c.head_dim
-    _need(v.shape == k.shape and (q is None) == (q_out is None), "k and v have as many rows; q comes with q_out")
-    qr = qo = ko = None
+    ops, dev = _operators(), _device(k)
+    c, seqs, h, d = _cache(ops, k_pages, v_pages, pages, dev)
+    n, dtype, i32 = k.shape[0], k_pages.dtype, ops.torch.int32
+    kr, vr = _token_rows(k, dev, dtype, n, h, d, "k"), _token_rows(v, dev, dtype, n, h, d, "v")
+    qr = qo = ko = starts = None
     heads = 0
-    if n == 0:  # (an empty tensor has no address to name)
-        return
+    if (q is None) != (q_out is None):
+        _bad("q comes with q_out")
     if q is not None:
-        _need(q.dim() == 3 and q.shape[0] == n and q_out.shape == q.shape, "q and q_out have as many rows as k")
-        heads = q.shape[1]
-        qr, qo = _token_rows(q, k_pages, heads, d, "q"), _token_rows(q_out, k_pages, heads, d, "q_out")
+        heads = q.shape[1] if q.dim() == 3 else 0
+        qr, qo = _token_rows(q, dev, dtype, n, heads, d, "q"), _token_rows(q_out, dev, dtype, n, heads, d, "q_out")
     if k_out is not None:
-        _need(k_out.shape == k.shape, "k_out has as many rows as k")
-        ko = _token_rows(k_out, k_pages, h, d, "k_out")
-    _call(k, lib().he_paged_append, c, rope, qr, heads, qo, _token_rows(k, k_pages, h, d, "k"), ko, _token_rows(v, k_pages, h, d, "v"),
-          None if seq_starts is None else _ints(seq_starts, (seqs + 1,), "seq_starts"), _ints(lens, (seqs,), "lens"), seqs, n)
+        ko = _token_rows(k_out, dev, dtype, n, h, d, "k_out")
+    if seq_starts is not None:
+        starts = _plain(ops, seq_starts, dev, i32, seqs + 1, "seq_starts")
+    at = _plain(ops, lens, dev, i32, seqs, "lens")
+    if n:  # (an empty tensor has no address to name)
+        ops.call(dev, ops.append, c, None if rope is None else C.addressof(rope), qr, heads, qo, kr, ko, vr, starts, at, seqs, n)
 
 
 def he_paged_attention_workspace(k_pages, v_pages, pages, heads: int, max_len: int = 0) -> int:
     """Bytes of workspace that he_paged_attention needs for as many sequences as the page table has."""
-    return lib().he_paged_attention_workspace(_cache(k_pages, v_pages, pages), heads, pages.shape[0], max_len)
+    ops = _operators()
+    c, seqs, _, _ = _cache(ops, k_pages, v_pages, pages, _device(k_pages))
+    return ops.workspace(c, heads, seqs, max_len)
 
 
 def he_paged_attention(q, k_pages, v_pages, pages, lens, max_len: int = 0, scale: Optional[float] = None, out=None, workspace=None):
     """One token per sequence, q [sequences, heads, dim], over the first lens[b] positions of its pages; scale: dim^-0.5 unless given.  workspace: a
     tensor of he_paged_attention_workspace bytes for a program that keeps one."""
-    import torch
-    _on(q, k_pages, v_pages, pages, lens, out, workspace)
-    c = _cache(k_pages, v_pages, pages)
-    seqs, d = pages.shape[0], c.head_dim
-    _need(q.dim() == 3 and q.shape[0] == seqs, "q is [sequences, heads, dim]")
-    heads = q.shape[1]
+    ops, dev = _operators(), _device(q)
+    c, seqs, _, d = _cache(ops, k_pages, v_pages, pages, dev)
+    heads, dtype = q.shape[1] if q.dim() == 3 else 0, k_pages.dtype
+    qr = _token_rows(q, dev, dtype, seqs, heads, d, "q")
     if out is None:
-        out = torch.empty(seqs, heads, d, dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape, "out has the shape of q")
+        out = ops.torch.empty(seqs, heads, d, dtype=dtype, device=q.device)
+    o = _token_rows(out, dev, dtype, seqs, heads, d, "out")
+    at = _plain(ops, lens, dev, ops.torch.int32, seqs, "lens")
     if seqs == 0:
         return out
-    nbytes = lib().he_paged_attention_workspace(c, heads, seqs, max_len)
-    if workspace is None and nbytes:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    have = 0
-    if workspace is not None:
-        _need(workspace.is_contiguous(), "workspace is contiguous")
-        have = workspace.numel() * workspace.element_size()
-    _call(q, lib().he_paged_attention, c, _token_rows(q, k_pages, heads, d, "q"), heads, _token_rows(out, k_pages, heads, d, "out"), _ints(lens, (seqs,), "lens"),
-          seqs, max_len, d ** -0.5 if scale is None else scale, _ptr(workspace), have)
+    ws, have = None, 0
+    if workspace is None:
+        have = ops.workspace(c, heads, seqs, max_len)
+        if have:
+            workspace = ops.torch.empty(have, dtype=ops.torch.uint8, device=q.device)
+            ws = workspace.data_ptr()
+    else:
+        if not workspace.is_contiguous() or workspace.get_device() != dev:
+            _bad(f"workspace is contiguous, on device {dev}")
+        ws, have = workspace.data_ptr(), workspace.nbytes
+    ops.call(dev, ops.paged, c, qr, heads, o, at, seqs, max_len, d ** -0.5 if scale is None else scale, ws, have)
     return out
 
 
 def he_packed_attention(q, k, v, seq_starts, causal: bool = True, scale: Optional[float] = None, out=None):
     """Prompts laid end to end: q [n, heads, dim], k and v [n, kv heads, dim], sequence b in rows seq_starts[b] .. seq_starts[b + 1] - 1."""
-    import torch
-    _on(q, k, v, seq_starts, out)
-    _need(q.dim() == 3 and k.dim() == 3 and v.shape == k.shape and k.shape[0] == q.shape[0], "q is [n, heads, dim], k and v [n, kv heads, dim]")
+    ops, dev = _operators(), _device(q)
+    if q.dim() != 3 or k.dim() != 3:
+        _bad("q is [n, heads, dim], k and v [n, kv heads, dim]")
     n, heads, d = q.shape
+    hk, dtype = k.shape[1], q.dtype
+    qr, kr, vr = (_token_rows(t, dev, dtype, n, h, d, name) for t, h, name in ((q, heads, "q"), (k, hk, "k"), (v, hk, "v")))
     if out is None:
-        out = torch.empty(n, heads, d, dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape, "out has the shape of q")
-    _need(seq_starts.dim() == 1 and seq_starts.shape[0] >= 1, "seq_starts is [sequences + 1]")
-    seqs, hk = seq_starts.shape[0] - 1, k.shape[1]
-    if n == 0:
-        return out
-    _call(q, lib().he_packed_attention, _dtype(q), _token_rows(q, q, heads, d, "q"), heads, _token_rows(k, q, hk, d, "k"), _token_rows(v, q, hk, d, "v"), hk, d,
-          _token_rows(out, q, heads, d, "out"), _ints(seq_starts, (seqs + 1,), "seq_starts"), seqs, n, 1 if causal else 0, d ** -0.5 if scale is None else scale)
+        out = ops.torch.empty(n, heads, d, dtype=dtype, device=q.device)
+    o = _token_rows(out, dev, dtype, n, heads, d, "out")
+    seqs = seq_starts.numel() - 1
+    starts = _plain(ops, seq_starts, dev, ops.torch.int32, seqs + 1, "seq_starts")
+    if seqs < 0:
+        _bad("seq_starts holds the sequences' starts and the end of the last")
+    if n:
+        ops.call(dev, ops.packed, _code(ops, q), qr, heads, kr, vr, hk, d, o, starts, seqs, n, 1 if causal else 0, d ** -0.5 if scale is None else scale)
     return out
 
 
 def he_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
     """(ids int32 [rows], log-probabilities float32 [rows]) of a token per row of logits [rows, vocab], from the numbers uniform [rows] in [0, 1);
     the filters are tensors of a value per row, or None."""
-    import torch
-    _on(logits, uniform, temperature, top_k, top_p, min_p)
-    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits are [rows, vocab], a row contiguous")
+    ops, dev = _operators(), _device(logits)
+    torch = ops.torch
+    if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] != 1):
+        _bad("logits are [rows, vocab], a row contiguous")
     rows, vocab = logits.shape
+    f32 = torch.float32
+    u = _plain(ops, uniform, dev, f32, rows, "uniform")
+    f = None
+    if temperature is not None or top_k is not None or top_p is not None or min_p is not None:
+        f = _FILTERS(0 if temperature is None else _plain(ops, temperature, dev, f32, rows, "temperature"),
+                     0 if top_k is None else _plain(ops, top_k, dev, torch.int32, rows, "top_k"), 0 if top_p is None else _plain(ops, top_p, dev, f32, rows, "top_p"),
+                     0 if min_p is None else _plain(ops, min_p, dev, f32, rows, "min_p"))
     ids = torch.empty(rows, dtype=torch.int32, device=logits.device)
-    logprobs = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    if rows == 0:
-        return ids, logprobs
-    _need(uniform is not None, "uniform is needed")
-    f = he_filters(_floats(temperature, rows, "temperature"), None if top_k is None else _ints(top_k, (rows,), "top_k"), _floats(top_p, rows, "top_p"),
-                   _floats(min_p, rows, "min_p"))
-    _call(logits, lib().he_sample, _dtype(logits), he_rows(logits.data_ptr(), logits.stride(0)), rows, vocab, f, _floats(uniform, rows, "uniform"),
-          ids.data_ptr(), logprobs.data_ptr())
+    logprobs = torch.empty(rows, dtype=f32, device=logits.device)
+    if rows:
+        ops.call(dev, ops.sample, _code(ops, logits), _ROWS(logits.data_ptr(), logits.stride(0)), rows, vocab, f, u, ids.data_ptr(), logprobs.data_ptr())
     return ids, logprobs
