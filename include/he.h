@@ -345,14 +345,16 @@ he_status he_packed_attention(he_dtype dtype, const he_rows* q, int n_heads, con
  * the untempered, unfiltered row.  Any of the arrays may be NULL, as filters_opt itself: T = 1, and that filter off; a top_k outside
  * 1 .. vocab - 1, a top_p of 1 or more and a min_p of 0 or less are off as well; T of 0 or less, or NaN, takes the largest z, of equal
  * ones the lowest id.  A NaN logit counts as -infinity, which is never drawn; a row of nothing else gets id -1 and log-probability
- * -infinity.  Sums are taken in 64 bits: the id does not depend on their order. */
+ * -infinity.  Weights and their sums have 64 bits, and the same call gives the same id every time.  d_workspace:
+ * he_sample_workspace(rows, vocab) bytes of any contents, one to every call that may run at the same time.  65535 rows at most. */
 typedef struct {
     const float* d_temperature; /* [rows] each, or NULL */
     const int32_t* d_top_k;
     const float *d_top_p, *d_min_p;
 } he_filters;
+size_t he_sample_workspace(int rows, int vocab);
 he_status he_sample(he_dtype dtype, const he_rows* logits, int rows, int vocab, const he_filters* filters_opt, const float* d_uniform, int32_t* d_ids,
-                    float* d_logprobs, void* stream);
+                    float* d_logprobs, void* d_workspace, size_t workspace_bytes, void* stream);
 
 /* Empties the KV cache (lengths to zero; memory is kept). */
 he_status he_reset(he_engine* e);

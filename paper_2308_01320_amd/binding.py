@@ -188,7 +188,9 @@ def lib() -> C.CDLL:
     L.he_packed_attention.restype = C.c_int
     L.he_packed_attention.argtypes = [C.c_int, rows, C.c_int, rows, rows, C.c_int, C.c_int, rows, ip, C.c_int, C.c_int, C.c_int, C.c_float, vp]
     L.he_sample.restype = C.c_int
-    L.he_sample.argtypes = [C.c_int, rows, C.c_int, C.c_int, C.POINTER(he_filters), fp, ip, fp, vp]
+    L.he_sample_workspace.restype = C.c_size_t
+    L.he_sample_workspace.argtypes = [C.c_int, C.c_int]
+    L.he_sample.argtypes = [C.c_int, rows, C.c_int, C.c_int, C.POINTER(he_filters), fp, ip, fp, vp, C.c_size_t, vp]
     _lib = L
     return L
 
@@ -202,7 +204,7 @@ EXPORTS = ("he_workspace_bytes", "he_create", "he_refresh_weights", "he_prefill"
            "he_decode_scratch_account", "he_arrival_counters_nonzero", "he_arrival_counters_set", "he_last_step_rows",
            "he_plan_prompt_gemm", "he_plan_pass_gemm", "he_plan_attention", "he_plan_plain_gemm", "he_plan_weight_copies",
            "he_plan_fetch_ahead", "he_operator_error", "he_paged_append", "he_paged_attention_workspace", "he_paged_attention",
-           "he_packed_attention", "he_sample")
+           "he_packed_attention", "he_sample_workspace", "he_sample")
 
 KERNEL_CLASSES = ("layernorm", "qkv", "attention", "out_proj", "fc1", "fc2", "lm_head", "empty")
 
@@ -594,7 +596,8 @@ class _Operators:
         self.workspace = entry("he_paged_attention_workspace", p, i, i, i, restype=C.c_size_t)
         self.paged = entry("he_paged_attention", p, p, i, p, p, i, i, C.c_float, p, C.c_size_t, p)
         self.packed = entry("he_packed_attention", i, p, i, p, p, i, i, p, p, i, i, i, C.c_float, p)
-        self.sample = entry("he_sample", i, p, i, i, p, p, p, p, p)
+        self.sample_workspace = entry("he_sample_workspace", i, i, restype=C.c_size_t)
+        self.sample = entry("he_sample", i, p, i, i, p, p, p, p, p, C.c_size_t, p)
 
     def call(self, dev, entry, *args):
         if self.device() != dev:
@@ -693,6 +696,11 @@ def he_paged_append(k, v, k_pages, v_pages, pages, lens, seq_starts=None, q=None
         ops.call(dev, ops.append, c, None if rope is None else C.addressof(rope), qr, heads, qo, kr, ko, vr, starts, at, seqs, n)
 
 
+def he_sample_workspace(rows: int, vocab: int) -> int:
+    """Bytes of workspace that he_sample needs."""
+    return lib().he_sample_workspace(rows, vocab)
+
+
 def he_paged_attention_workspace(k_pages, v_pages, pages, heads: int, max_len: int = 0) -> int:
     """Bytes of workspace that he_paged_attention needs for as many sequences as the page table has."""
     ops = _operators()
@@ -747,9 +755,9 @@ def he_packed_attention(q, k, v, seq_starts, causal: bool = True, scale: Optiona
     return out
 
 
-def he_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
+def he_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None):
     """(ids int32 [rows], log-probabilities float32 [rows]) of a token per row of logits [rows, vocab], from the numbers uniform [rows] in [0, 1);
-    the filters are tensors of a value per row, or None."""
+    the filters are tensors of a value per row, or None.  workspace: a tensor of he_sample_workspace bytes for a program that keeps one."""
     ops, dev = _operators(), _device(logits)
     torch = ops.torch
     if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] != 1):
@@ -765,5 +773,10 @@ def he_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=N
     ids = torch.empty(rows, dtype=torch.int32, device=logits.device)
     logprobs = torch.empty(rows, dtype=f32, device=logits.device)
     if rows:
-        ops.call(dev, ops.sample, _code(ops, logits), _ROWS(logits.data_ptr(), logits.stride(0)), rows, vocab, f, u, ids.data_ptr(), logprobs.data_ptr())
+        if workspace is None:
+            workspace = torch.empty(ops.sample_workspace(rows, vocab), dtype=torch.uint8, device=logits.device)
+        elif not workspace.is_contiguous() or workspace.get_device() != dev:
+            _bad(f"workspace is contiguous, on device {dev}")
+        ops.call(dev, ops.sample, _code(ops, logits), _ROWS(logits.data_ptr(), logits.stride(0)), rows, vocab, f, u, ids.data_ptr(), logprobs.data_ptr(),
+                 workspace.data_ptr(), workspace.nbytes)
     return ids, logprobs

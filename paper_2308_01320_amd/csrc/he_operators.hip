@@ -173,18 +173,23 @@ he_status he_packed_attention(he_dtype dtype, const he_rows* q, int n_heads, con
     return launched();
 }
 
+size_t he_sample_workspace(int rows, int vocab) { return rows < 1 || rows > 65535 || vocab < 1 || vocab > 1 << 20 ? 0 : sample_workspace(rows, vocab); }
+
 he_status he_sample(he_dtype dtype, const he_rows* logits, int rows, int vocab, const he_filters* filters_opt, const float* d_uniform, int32_t* d_ids,
-                    float* d_logprobs, void* stream) {
+                    float* d_logprobs, void* d_workspace, size_t workspace_bytes, void* stream) {
     if (!known(dtype)) return refuse(HE_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
     if (!logits || !logits->data || !d_uniform || !d_ids || !d_logprobs) return refuse(HE_ERR_INVALID_ARG, "logits, d_uniform, d_ids or d_logprobs is NULL");
     if ((uintptr_t)logits->data % elt_bytes(dtype)) return refuse(HE_ERR_SHAPE, "logits do not lie on whole elements");
     if (rows < 0 || vocab < 1) return refuse(HE_ERR_INVALID_ARG, "%d rows of %d logits", rows, vocab);
     if (vocab > 1 << 20) return refuse(HE_ERR_SHAPE, "vocabulary of %d: 2^20 at most", vocab);
-    if (rows > kMost) return refuse(HE_ERR_SHAPE, "over 2^30 rows");
+    if (rows > 65535) return refuse(HE_ERR_SHAPE, "%d rows: 65535 at most", rows);
     if (logits->stride < 0) return refuse(HE_ERR_SHAPE, "logits: rows %lld elements apart", (long long)logits->stride);
     if (rows == 0) return HE_OK;
+    const size_t need = sample_workspace(rows, vocab);
+    if (!d_workspace || workspace_bytes < need) return refuse(HE_ERR_CAPACITY, "workspace of %zu bytes, %zu are needed", d_workspace ? workspace_bytes : (size_t)0, need);
+    if (!aligned(d_workspace)) return refuse(HE_ERR_SHAPE, "workspace does not lie on 16 bytes");
     const Filters f = filters_opt ? Filters{filters_opt->d_temperature, filters_opt->d_top_k, filters_opt->d_top_p, filters_opt->d_min_p} : Filters{};
-    sample((hipStream_t)stream, dtype, device_rows(logits), rows, vocab, f, d_uniform, d_ids, d_logprobs);
+    sample((hipStream_t)stream, dtype, device_rows(logits), rows, vocab, f, d_uniform, d_ids, d_logprobs, d_workspace);
     return launched();
 }
 

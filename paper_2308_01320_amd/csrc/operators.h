@@ -114,6 +114,8 @@ void packed_attention(hipStream_t s, he_dtype dt, Rows q, int n_heads, Rows k, R
                       const int32_t* starts, int n_seqs, int n_tokens, bool causal, float scale);
 
 struct Filters { const float* temperature; const int32_t* top_k; const float *top_p, *min_p; };
-void sample(hipStream_t s, he_dtype dt, Rows logits, int rows, int vocab, const Filters& f, const float* uniform, int32_t* ids, float* logprobs);
+size_t sample_workspace(int rows, int vocab);
+void sample(hipStream_t s, he_dtype dt, Rows logits, int rows, int vocab, const Filters& f, const float* uniform, int32_t* ids, float* logprobs,
+            void* workspace);
 
 }  // namespace he_op

@@ -34,8 +34,8 @@ def packed(dtype=B.HE_F16, q=None, heads=4, k=None, v=None, kv=2, d=64, out=None
                                        rows() if out is None else out, starts, seqs, n, causal, scale, None)
 
 
-def sample(dtype=B.HE_F32, z=None, n=2, vocab=100, f=None, u=P, ids=P, lp=P):
-    return B.lib().he_sample(dtype, rows() if z is None else z, n, vocab, f, u, ids, lp, None)
+def sample(dtype=B.HE_F32, z=None, n=2, vocab=100, f=None, u=P, ids=P, lp=P, ws=P, nbytes=1 << 30):
+    return B.lib().he_sample(dtype, rows() if z is None else z, n, vocab, f, u, ids, lp, ws, nbytes, None)
 
 
 BAD_CACHES = [
@@ -98,6 +98,9 @@ def test_packed_attention_refuses():
 def test_sample_refuses():
     assert sample(dtype=9) == sample(n=-1) == sample(vocab=0) == 1
     assert sample(vocab=(1 << 20) + 1) == sample(z=rows(P + 2)) == sample(z=rows(stride=-1)) == 2
+    assert sample(n=65536) == 2 and sample(ws=P + 8) == 2
+    need = B.he_sample_workspace(2, 100)
+    assert need > 0 and sample(nbytes=need - 1) == sample(ws=None) == 3 and B.he_sample_workspace(0, 5) == B.he_sample_workspace(1, (1 << 20) + 1) == 0
     assert sample(n=0) == 0
 
 
