@@ -25,7 +25,8 @@ constexpr int kStep = 4, kBins = ((kUnit + 1024) >> kStep) + 1;  // steps of 2^k
 constexpr int kList = 2048;                     // tokens of a step that are compared one with another
 constexpr int kHead = 8192;                     // tokens of a row's head
 constexpr int kSpans = kThreads;                // spans of ids
-constexpr int kSlice = 4096, kSliceThreads = 256, kSliceHead = 1024;
+constexpr int kSlice = 4096, kSliceThreads = 256, kSliceHead = 2048;
+constexpr int kAllHead = 512;                   // a vocabulary of no more is all head
 static_assert((1 << 20) / kSlice <= kThreads, "a thread to a slice of the longest row");
 
 // A token's place in the order as one number: a larger place comes first.
@@ -378,10 +379,10 @@ __device__ __forceinline__ Limit limit_of(Shared& sh, const Source& src, const A
 // ---- the slices
 //
 // What a slice's workgroup leaves.  soft, rest, mass: sums of exp(z - largest) and of exp((z - largest) / T) -- soft and rest over the tokens below
-// `cut` (soft over all of them where the head did not fit and is left out), mass, of a row without filters, over all of them.
+// `cut`, mass, of a row without filters, over all of them.
 struct Slice {
     float largest, cut;
-    int n, whole;  // tokens of the head; whole: it did not fit
+    int n, whole;  // tokens of the head; whole: it did not fit, and the row is gone over as a whole
     double soft, rest, mass;
 };
 struct Workspace {
@@ -413,7 +414,7 @@ __device__ __forceinline__ RowFilters filters_of(const Filters& f, int r, int vo
     a.first_only = a.k == 1 || !(a.temperature > 0.f) || a.p <= 0.f || a.least > 1.f;
     a.top_k = !a.first_only && a.k > 1 && a.k < vocab;
     a.top_p = !a.first_only && a.p < 1.f;
-    a.any = a.first_only || a.top_k || a.top_p || a.least > 0.f || vocab <= kSliceHead;  // (a row that is all head)
+    a.any = a.first_only || a.top_k || a.top_p || a.least > 0.f || vocab <= kAllHead;  // (a row that is all head)
     return a;
 }
 
@@ -443,9 +444,14 @@ __global__ __launch_bounds__(kSliceThreads) void slice_kernel(Rows logits, int v
     }
 #pragma unroll
     for (int i = 0; i < P * N; ++i) best = fmaxf(best, x[i]);
-    // Each of 128 groups of the slice's tokens has one at `cut` or above it: some 128 (ln 128 + 0.6) = 700, if they lie in no particular order.
-    // Groups of nothing but -infinity do not count.
-    const float of_two = lane_max<2>(best), other = lane_max<64>(of_two > -INFINITY ? -of_two : -INFINITY);
+    // Each of 128 groups of the slice's tokens has one at `cut` or above it: some 128 (ln 128 + 0.6) = 700, if they lie in no particular order, and hardly
+    // ever three times as many.  (Fewer groups to each of many slices, so that a row's heads together fit into LDS.)  Groups of nothing but
+    // -infinity do not count.
+    float of_group = lane_max<2>(best);
+    if (gridDim.x > 16) of_group = fmaxf(of_group, lane_xor2(of_group));
+    if (gridDim.x > 32) of_group = fmaxf(of_group, lane_mirror8(of_group));
+    if (gridDim.x > 64) of_group = fmaxf(of_group, lane_mirror16(of_group));
+    const float other = lane_max<64>(of_group > -INFINITY ? -of_group : -INFINITY);
     best = lane_max<64>(best);
     if (lane == 0) { sh_max[wave] = best; sh_cut[wave] = other; }
     __syncthreads();
@@ -453,7 +459,7 @@ __global__ __launch_bounds__(kSliceThreads) void slice_kernel(Rows logits, int v
 #pragma unroll
     for (int i = 1; i < W; ++i) { largest = fmaxf(largest, sh_max[i]); cut = fmaxf(cut, sh_cut[i]); }
     cut = -cut;  // (+infinity where there is nothing)
-    if (vocab <= kSliceHead) cut = -INFINITY;
+    if (vocab <= kAllHead) cut = -INFINITY;
     if (largest == INFINITY) cut = INFINITY;
     int mine = 0;
     uint32_t in_head = 0;
@@ -491,10 +497,7 @@ __global__ __launch_bounds__(kSliceThreads) void slice_kernel(Rows logits, int v
     double soft = 0.0, rest = 0.0, mass = 0.0;
     if (largest > -INFINITY && largest < INFINITY) {
         const double rate = 1.4426950408889634 / (double)ask.temperature;
-        if (whole) {
-#pragma unroll
-            for (int i = 0; i < P * N; ++i) soft += exp2(((double)x[i] - (double)largest) * 1.4426950408889634);
-        } else {
+        if (!whole) {
             const float hi = (float)rate, lo = (float)(rate - (double)hi);
             float s = 0.f, t = 0.f;
 #pragma unroll
@@ -515,7 +518,6 @@ __global__ __launch_bounds__(kSliceThreads) void slice_kernel(Rows logits, int v
                 mass += e >= -43.0 ? exp2(e) : 0.0;  // (no NaN of -infinity times nothing, and none that weighs nothing against the row's largest)
             }
     } else if (largest == INFINITY) {  // so many of one weight, and nothing else
-        soft = whole ? (double)mine : 0.0;
         mass = (double)mine;
     }
     const auto addd = [](double a, double b) { return a + b; };
@@ -576,64 +578,70 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Rows logits, int vocab
     const double rate = ask.rate = rf.first_only ? kPlain : kPlain / (double)rf.temperature;
 
     // the sums of what the slices' heads do not hold, and the heads: those from `cut` up into LDS, the others into the sums
-    double lse = 0.0;
-    if (some) lse = !row.infinite ? mine.soft * exp2(((double)mine.largest - top) * (kPlain / 1024.0)) : mine.largest == INFINITY ? mine.soft : 0.0;
+    double lse = some && !row.infinite ? mine.soft * exp2(((double)mine.largest - top) * (kPlain / 1024.0)) : 0.0;
     double rest = some && !row.infinite && ask.top_p ? mine.rest * exp2(((double)mine.largest - top) * (rate / 1024.0)) : 0.0;
     int first = INT_MAX;
-    // (two slices at a time, two tokens of each to a thread, the next two's on their way)
-    float next_x[4];
-    int next_id[4];
-    auto request = [&](int s0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int slice = s0 + (i >> 1), in = (i & 1) * kThreads + threadIdx.x;
-            const bool have = slice < n_slices && in < sh.slice_n[min(slice, n_slices - 1)];
-            const size_t at = ((size_t)r * n_slices + slice) * kSliceHead + in;
-            next_x[i] = have ? ws.logit[at] : -INFINITY;
-            next_id[i] = have ? ws.id[at] : 0;
-        }
-    };
-    static_assert(2 * kThreads == kSliceHead, "two tokens of each slice's head to a thread");
-    request(0);
+    // (a slice to a wavefront, sixteen tokens to a lane on their way together; those below the cut count in float, like the slices' sums)
+    const float rate_hi = (float)(rate / 1024.0), rate_lo = (float)(rate / 1024.0 - (double)rate_hi);
 #pragma unroll 1
-    for (int s0 = 0; s0 < n_slices; s0 += 2) {
-        float x[4];
-        int id[4];
+    for (int s = wave; s < n_slices; s += kWaves) {
+        constexpr int B = 16;
+        const int n = sh.slice_n[s];
+        const size_t at = ((size_t)r * n_slices + s) * kSliceHead + lane;
+        float soft_part = 0.f, rest_part = 0.f;
+#pragma unroll 1
+        for (int i0 = 0; i0 < n; i0 += B * 64) {
+            float x[B];
+            int id[B];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = !row.infinite ? next_x[i] : next_x[i] == INFINITY ? 0.f : -INFINITY;
-            id[i] = next_id[i];
-        }
-        request(s0 + 2);
-        Log l[4];
-        unsigned long long w[4];
-        weights<4>(x, top, kPlain, sh.pow2, l, w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) lse += (double)w[i] * 0x1p-42;
-        if (ask.top_p) {
-            weights<4>(x, top, rate, sh.pow2, l, w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) rest += x[i] < cut ? (double)w[i] * 0x1p-42 : 0.0;
-        }
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) n += x[i] >= cut && x[i] > -INFINITY ? 1 : 0;
-        int upto = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(upto, o);
-            if (lane >= o) upto += v;
-        }
-        int base = 0;
-        if (lane == 63) base = atomicAdd(&sh.head_n, upto);
-        base = __builtin_amdgcn_readlane(base, 63) + upto - n;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (x[i] >= cut && x[i] > -INFINITY) {
-                if (base < kHead) { sh.head_logit[base] = x[i]; sh.head_id[base] = id[i]; }
-                ++base;
-                if (x[i] == ask.topf) first = min(first, id[i]);
+            for (int i = 0; i < B; ++i) {
+                const bool have = i0 + i * 64 + lane < n;
+                x[i] = have ? ws.logit[at + i0 + i * 64] : -INFINITY;
+                id[i] = have ? ws.id[at + i0 + i * 64] : 0;
             }
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                if (row.infinite) x[i] = x[i] == INFINITY ? 0.f : -INFINITY;
+                const bool in = x[i] >= cut && x[i] > -INFINITY;
+                const float d = fmaxf(x[i] - ask.topf, -3e38f);
+                const float a = __builtin_amdgcn_exp2f(fmaf(d, 1.44269502f, d * 1.92596299e-8f));
+                soft_part += in ? 0.f : a;
+                if (ask.top_p) {
+                    const float t = __builtin_amdgcn_exp2f(fmaf(d, rate_hi, d * rate_lo));
+                    rest_part += in ? 0.f : t;
+                }
+                const uint64_t who = __ballot(in);
+                int base = 0;
+                if (lane == 0) base = atomicAdd(&sh.head_n, __popcll(who));
+                base = __builtin_amdgcn_readfirstlane(base) + __popcll(who & ((1ull << lane) - 1));
+                if (in && base < kHead) { sh.head_logit[base] = x[i]; sh.head_id[base] = id[i]; }
+                if (in && x[i] == ask.topf) first = min(first, id[i]);
+            }
+        }
+        lse += (double)soft_part;
+        rest += (double)rest_part;
+    }
+    __syncthreads();
+    Head head{&sh, min(sh.head_n, kHead)};
+    const bool whole_head = !whole && sh.head_n <= kHead;
+    // the head's own part of the soft-max's sum: a few large terms can be all of it
+    if (whole_head) {
+        head.each([&](const int (&)[4], const float (&x)[4]) {
+            Log l[4];
+            unsigned long long w[4];
+            weights<4>(x, top, kPlain, sh.pow2, l, w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lse += (double)w[i] * 0x1p-42;
+        });
+    } else {  // (it does not fit: all of the row)
+        lse = 0.0;
+        row.each([&](const int (&)[8], const float (&x)[8]) {
+            Log l[8];
+            unsigned long long w[8];
+            weights<8>(x, top, kPlain, sh.pow2, l, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) lse += (double)w[i] * 0x1p-42;
+        });
     }
     lse = block_all(lse, sh.wave_d, addd);
     rest = block_all(rest, sh.wave_d, addd);
@@ -705,12 +713,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Rows logits, int vocab
         }
     } else {
         Limit lim{-INFINITY, INT_MAX, false};
-        Head head{&sh, sh.head_n};
         bool by_head = false;
         if (rf.first_only) {
             lim.z = ask.topf;  // (more than fit of one value or little else: its first, below)
         } else {
-            if (!whole && head.n <= kHead && rate < 1e30) {  // (a temperature next to nothing: the rest's weights are no floats)
+            if (whole_head && rate < 1e30) {  // (a temperature next to nothing: the rest's weights are no floats)
                 const bool complete = log_weight(cut, top, rate).zero;
                 lim = limit_of(sh, head, ask, (unsigned long long)(rest * 4398046511104.0), complete, cut);
                 by_head = lim.all;
@@ -731,6 +738,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Rows logits, int vocab
             __syncthreads();
             int final = -1;
             head.each([&](const int (&i)[4], const float (&x)[4]) {
+                if (fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) < lim.z) return;
                 Log l[4];
                 unsigned long long w[4];
                 weights<4>(x, top, rate, sh.pow2, l, w);
