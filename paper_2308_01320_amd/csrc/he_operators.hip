@@ -83,7 +83,7 @@ int longest_of(const he_paged_cache& c, int max_len) {
     return max_len < 1 || max_len > all ? all : max_len;
 }
 size_t split_bytes(int n_seqs, int n_heads, int d, int splits) {
-    return splits > 1 ? (size_t)n_seqs * n_heads * splits * (d + 2) * sizeof(float) : 0;
+    return splits > 1 ? (size_t)n_seqs * n_heads * splits * (d + 2) * sizeof(float) + 16 : 0;  // (values on 16 bytes behind maxima and sums)
 }
 
 }  // namespace

@@ -41,11 +41,13 @@ __device__ __forceinline__ f32x16 mma(const Operand<F32>& a, const Operand<F32>&
 
 // The tiles: rows of DP values (d rounded up; the pieces past d hold another of the row's, which nothing uses) as 16-byte pieces, piece c of row r at
 // place c ^ turn(r): the rows' starts alone would put a column of pieces on few banks.
-template <class E, int DP>
+// SPLIT: the wavefronts of a workgroup have the same queries and 32 keys each of every tile.
+template <class E, int DP, int WAVES, bool SPLIT>
 struct Tiles {
     typedef typename E::T T;
-    static constexpr int N = 16 / sizeof(T), CPR = DP / N;           // values of a piece, pieces of a row
-    static constexpr int BN = DP * sizeof(T) <= 256 ? 64 : 32;       // keys of a tile
+    static constexpr int N = 16 / sizeof(T), CPR = DP / N;                               // values of a piece, pieces of a row
+    static constexpr int BN = SPLIT ? 32 * WAVES : DP * sizeof(T) <= 256 ? 64 : 32;      // keys of a tile
+    static constexpr int ROWS = SPLIT ? 32 : 32 * WAVES;                                 // queries of a workgroup
     static constexpr int BYTES = BN * DP * sizeof(T);
     static __device__ __forceinline__ int k_turn(int r) { return CPR >= 16 ? r & 15 : (r >> 1) & 7; }
     // (transposing reads take two pieces of four rows at a time, float reads a row of 32 values)
@@ -191,25 +193,25 @@ __device__ __forceinline__ void one_query(const PackedArgs& p, int h, int hk, in
 }
 
 // EXACT: the head dimension is DP
-template <class E, int DP, bool EXACT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DP * sizeof(typename E::T) <= 256 ? 2 : 1) void packed_attention_kernel(PackedArgs p) {
+template <class E, int DP, bool EXACT, int WAVES, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES, !SPLIT && DP * sizeof(typename E::T) <= 256 ? 2 : 1) void packed_attention_kernel(PackedArgs p) {
     typedef typename E::T T;
-    typedef Tiles<E, DP> Ti;
-    constexpr int BN = Ti::BN, SUB = BN / 32, KBD = DP / 16, DB = DP / 32, LOADS = BN * Ti::CPR / (64 * WAVES);
+    typedef Tiles<E, DP, WAVES, SPLIT> Ti;
+    constexpr int BN = Ti::BN, SUB = SPLIT ? 1 : BN / 32, KBD = DP / 16, DB = DP / 32, LOADS = BN * Ti::CPR / (64 * WAVES);
     static_assert(LOADS * 64 * WAVES == BN * Ti::CPR, "whole pieces to a thread");
     extern __shared__ __align__(1024) unsigned char smem[];  // two buffers of K and V tiles
     const int d = EXACT ? DP : p.d, share = p.n_heads / p.n_kv_heads;
     // heads that share keys follow each other eight (XCDs) or more apart where there are as many key-value heads, so a key-value head stays in one L2
     const int hq = blockIdx.x % p.n_heads, hk = hq % p.n_kv_heads, h = hk * share + hq / p.n_kv_heads;
     Seq seq;
-    if (!block_at(p.starts, p.n_seqs, p.n_tokens, 32 * WAVES, blockIdx.x / p.n_heads, seq)) return;  // (the whole workgroup)
+    if (!block_at(p.starts, p.n_seqs, p.n_tokens, Ti::ROWS, blockIdx.x / p.n_heads, seq)) return;  // (the whole workgroup)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 31, hh = lane >> 5;
-    const int q0 = seq.begin + (seq.block * WAVES + wave) * 32;  // this wavefront's first query
-    const int last_q = min(seq.end, seq.begin + (seq.block + 1) * WAVES * 32) - 1;
+    const int q0 = seq.begin + seq.block * Ti::ROWS + (SPLIT ? 0 : wave * 32);  // this wavefront's first query
+    const int last_q = min(seq.end, seq.begin + (seq.block + 1) * Ti::ROWS) - 1, sub0 = SPLIT ? wave * 32 : 0;  // ... and its part of a tile
     const int keys = (p.causal ? last_q + 1 : seq.end) - seq.begin, n_tiles = (keys + BN - 1) / BN;
     // the tiles this wavefront takes part in, and the first with keys that some query of it does not see
     const int my_keys = q0 >= seq.end ? 0 : p.causal ? min(q0 + 32, seq.end) - seq.begin : keys;
-    const int my_tiles = (my_keys + BN - 1) / BN, mask_from = p.causal ? (q0 - seq.begin + 1) / BN : (seq.end - seq.begin) / BN;
+    const int my_tiles = (my_keys - sub0 + BN - 1) / BN, mask_from = ((p.causal ? q0 - seq.begin + 1 : seq.end - seq.begin) - sub0) / BN;
     const int seen = (p.causal ? min(q0 + j + 1, seq.end) : seq.end) - seq.begin;  // keys this lane's query sees
     // The copies of a tile: piece s of it to lane s % 64; a lane's row moves on by RPN from copy to copy, and the turn of its pieces comes round
     // every PERIOD of them, so that what a copy adds to the lane's offset is the same for all lanes.
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(typename E::T) <= 256 ? 2 :
             f32x16 a = f32x16{};
 #pragma unroll
             for (int kb = 0; kb < KBD; ++kb) {
-                if (EXACT || kb * 16 < d) a = mma(Ti::k_operand(kt, x * 32 + j, kb, hh), KEEP ? q[KEEP ? kb : 0] : query(kb), a);
+                if (EXACT || kb * 16 < d) a = mma(Ti::k_operand(kt, sub0 + x * 32 + j, kb, hh), KEEP ? q[KEEP ? kb : 0] : query(kb), a);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[x][r] = a[r];
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(typename E::T) <= 256 ? 2 :
             for (int x = 0; x < SUB; ++x)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (tile * BN + x * 32 + 8 * (r >> 2) + 4 * hh + (r & 3) >= seen) s[x][r] = -INFINITY;
+                    if (tile * BN + sub0 + x * 32 + 8 * (r >> 2) + 4 * hh + (r & 3) >= seen) s[x][r] = -INFINITY;
         }
         float top = s[0][0];
 #pragma unroll
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(typename E::T) <= 256 ? 2 :
         }
         if constexpr (sizeof(T) == 2) {
             constexpr int G = DB < 4 ? DB : 4;  // blocks of dimensions whose values are read together
-            const uint32_t base = (uint32_t)((tile & 1) * 2 * Ti::BYTES + Ti::BYTES);
+            const uint32_t base = (uint32_t)((tile & 1) * 2 * Ti::BYTES + Ti::BYTES + sub0 * Ti::CPR * 16);
             auto step = [&](auto y) {
                 constexpr int Y = decltype(y)::value;
                 const Operand<E> w = weights8<E>(&s[Y >> 1][8 * (Y & 1)]);
@@ -358,12 +360,45 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(typename E::T) <= 256 ? 2 :
                 const Operand<E> w = weights8<E>(&s[y >> 1][8 * (y & 1)]);
 #pragma unroll
                 for (int i = 0; i < DB; ++i)
-                    if (EXACT || i * 32 < d) o[i] = mma(Ti::v_floats(vt, y * 16, i, lane), w, o[i]);
+                    if (EXACT || i * 32 < d) o[i] = mma(Ti::v_floats(vt, sub0 + y * 16, i, lane), w, o[i]);
+            }
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if constexpr (SPLIT && WAVES > 1) {
+        // the wavefronts' parts of the same queries, each on its own scale, added up in their order; a wavefront then has every WAVES-th block of
+        // dimensions
+        __shared__ float2 ml[WAVES][32];
+        __syncthreads();  // (the tiles' memory is free)
+        float* parts = reinterpret_cast<float*>(smem);
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) parts[((wave * DB + i) * 16 + r) * 64 + lane] = o[i][r];
+        if (hh == 0) ml[wave][j] = make_float2(m, l);
+        __syncthreads();
+        float top = -INFINITY, f[WAVES];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[w][j].x);
+        l = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float2 a = ml[w][j];
+            f[w] = a.x > -INFINITY ? __builtin_amdgcn_exp2f(a.x - top) : a.y;  // (nothing seen: 0; or a NaN)
+            l += a.y * f[w];
+        }
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float v = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) v = fmaf(parts[((w * DB + i) * 16 + r) * 64 + lane], f[w], v);
+                o[i][r] = v;
             }
         }
     }
     if (q0 >= seq.end) return;
-    l += __shfl_xor(l, 32);
     const float inv = 1.0f / l;
     bool fine = true;
 #pragma unroll
@@ -377,7 +412,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(typename E::T) <= 256 ? 2 :
     const bool mine = q0 + j < seq.end;
     if (__any(mine && !fine)) {  // infinities or NaN among the values: keep what a query does not see out of its sums
         const int n = min(32, seq.end - q0);
-        for (int i = 0; i < n; ++i) one_query<E, DP>(p, h, hk, q0 + i, seq.begin, p.causal ? q0 + i + 1 : seq.end);
+        for (int i = SPLIT ? wave : 0; i < n; i += SPLIT ? WAVES : 1) one_query<E, DP>(p, h, hk, q0 + i, seq.begin, p.causal ? q0 + i + 1 : seq.end);
         return;
     }
     T* op = (T*)p.out.data + (int64_t)(mine ? q0 + j : q0) * p.out.stride + (int64_t)h * d;
@@ -386,7 +421,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(typename E::T) <= 256 ? 2 :
 #pragma unroll
         for (int r = 0; r < 16; r += 8) {
             const int dim = i * 32 + 8 * (r >> 2);  // the lower lanes hold four from here and four from dim + 8, the upper the next four of each
-            if (!EXACT && dim >= d) continue;
+            if ((!EXACT && dim >= d) || (SPLIT && i % WAVES != wave)) continue;
             if constexpr (sizeof(T) == 2) {
                 uint32_t a0 = E::pack(o[i][r], o[i][r + 1]), a1 = E::pack(o[i][r + 2], o[i][r + 3]);
                 uint32_t b0 = E::pack(o[i][r + 4], o[i][r + 5]), b1 = E::pack(o[i][r + 6], o[i][r + 7]);
@@ -406,11 +441,26 @@ void packed_attention(hipStream_t s, he_dtype dt, Rows q, int n_heads, Rows k, R
     const PackedArgs args{q, k, v, out, starts, n_heads, n_kv_heads, head_dim, n_seqs, n_tokens, causal ? 1 : 0, scale};
     by_type(dt, [&](auto e) {
         typedef decltype(e) E;
+        // 128 queries to a workgroup, or 32 whose keys its wavefronts share out: where four times the workgroups fit the CUs at once (float: in three rounds, its
+        // products are sixteen times as long against the merge).  us, 128 -> 32 queries: half, 32 heads of 64, 250 tokens 8.5 -> 7.4; bf16,
+        // 4 heads of 64, 1500 tokens 26.3 -> 15.2, 8 of 256, 1000 tokens 69.8 -> 45.3, 32 of 128, 250 tokens 11.4 -> 10.6 but 500 tokens
+        // 17.2 -> 21.3; float, 8 heads of 64, 2000 tokens 147.7 -> 62.6, 32 of 64, 500 tokens 41.8 -> 26.5.
         auto launch = [&](auto dp, auto exact) {
-            constexpr int DP = decltype(dp)::value, WAVES = 4;
-            // a sequence has one block more than its rows fill at most
-            const unsigned blocks = (unsigned)(n_tokens / (32 * WAVES) + std::min(n_seqs, n_tokens));
-            packed_attention_kernel<E, DP, decltype(exact)::value, WAVES><<<blocks * n_heads, 64 * WAVES, 4 * Tiles<E, DP>::BYTES, s>>>(args);
+            constexpr int DP = decltype(dp)::value, TILE = 32 * DP * (int)sizeof(typename E::T) * 4;  // two buffers of 32 keys and values
+            constexpr int SHARE = TILE * 4 <= 131072 ? 4 : TILE * 2 <= 131072 ? 2 : 1;
+            auto run = [&](auto waves, auto shared) {
+                typedef Tiles<E, DP, decltype(waves)::value, decltype(shared)::value> Ti;
+                // a sequence has one block more than its rows fill at most
+                const unsigned blocks = (unsigned)(n_tokens / Ti::ROWS + std::min(n_seqs, n_tokens));
+                packed_attention_kernel<E, DP, decltype(exact)::value, decltype(waves)::value, decltype(shared)::value>
+                    <<<blocks * n_heads, 64 * decltype(waves)::value, 4 * Ti::BYTES, s>>>(args);
+            };
+            if constexpr (SHARE > 1) {  // (a tile of float rows of 256 is as much as LDS holds)
+                const int64_t at_once = (int64_t)he_bf16::num_cus() * (163840 / (TILE * SHARE + 1024)) * (sizeof(typename E::T) == 4 ? 3 : 1);
+                if ((int64_t)((n_tokens + 127) / 128) * n_heads * 4 <= at_once)
+                    return run(std::integral_constant<int, SHARE>{}, std::true_type{});
+            }
+            run(std::integral_constant<int, 4>{}, std::false_type{});
         };
         if (head_dim == 64) launch(std::integral_constant<int, 64>{}, std::true_type{});
         else if (head_dim == 128) launch(std::integral_constant<int, 128>{}, std::true_type{});

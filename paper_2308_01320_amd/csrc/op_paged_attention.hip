@@ -20,7 +20,7 @@ struct Partial {
     float* o;
 };
 __host__ __device__ inline Partial partial_of(float* workspace, size_t rows, int splits) {
-    return {reinterpret_cast<float2*>(workspace), workspace + 2 * rows * splits};
+    return {reinterpret_cast<float2*>(workspace), workspace + (2 * rows * splits + 3) / 4 * 4};
 }
 
 template <class E, int DP, int GQ>
@@ -290,35 +290,56 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_mma_kernel(Cache
     }
 }
 
-// The splits of a row, weighted by exp(their maximum - the largest)
+// The splits of a row, weighted by exp(their maximum - the largest): a split to a lane for the weights, then four dimensions to a thread and the
+// splits dealt out to as many groups of threads as there are, whose sums are added in their order.
+constexpr int kMostSplits = 64;
+
 template <class E>
 __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ workspace, Rows out, int n_heads, int d, int splits) {
     typedef typename E::T T;
-    const int row = blockIdx.x, b = row / n_heads, h = row % n_heads, e = threadIdx.x;
+    __shared__ float weight[kMostSplits];
+    __shared__ float4 part[256];
+    const int row = blockIdx.x, b = row / n_heads, h = row % n_heads, lane = threadIdx.x & 63;
     const Partial p = partial_of(const_cast<float*>(workspace), gridDim.x, splits);
-    float top = -INFINITY;
-    for (int s = 0; s < splits; ++s) top = fmaxf(top, p.ml[(size_t)row * splits + s].x);
-    float l = 0.f, o = 0.f;
-    for (int s = 0; s < splits; ++s) {
-        const float2 a = p.ml[(size_t)row * splits + s];
-        if (a.y == 0.f) continue;  // a split that saw no key
-        const float f = a.x > -INFINITY ? expf(a.x - top) : a.y;
-        l += a.y * f;
-        if (e < d) o += p.o[((size_t)row * splits + s) * d + e] * f;
+    const float2 a = lane < splits ? p.ml[(size_t)row * splits + lane] : make_float2(-INFINITY, 0.f);
+    const float top = lane_max<64>(a.x);
+    const float f = a.y == 0.f ? 0.f : a.x > -INFINITY ? expf(a.x - top) : a.y;  // (a split that saw no key; or a NaN)
+    const float l = lane_sum<64>(a.y == 0.f ? 0.f : a.y * f);
+    if (threadIdx.x < kMostSplits) weight[threadIdx.x] = f;
+    __syncthreads();
+    const int lanes = d >> 2, groups = 256 / lanes, e = threadIdx.x % lanes, g = threadIdx.x / lanes;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (g < groups) {
+#pragma unroll 4
+        for (int s = g; s < splits; s += groups) {
+            const float w = weight[s];
+            const float4 v = *reinterpret_cast<const float4*>(p.o + ((size_t)row * splits + s) * d + e * 4);
+            const bool some = w != 0.f;  // (else what lies there is no one's)
+            o.x += some ? v.x * w : 0.f;
+            o.y += some ? v.y * w : 0.f;
+            o.z += some ? v.z * w : 0.f;
+            o.w += some ? v.w * w : 0.f;
+        }
     }
-    if (e >= d) return;
-    const float y = attended(l, o), next = __shfl_xor(y, 1);
-    T* op = (T*)out.data + (int64_t)b * out.stride + (int64_t)h * d + e;
-    if constexpr (sizeof(T) == 4) *op = y;
-    else if (!(e & 1)) *reinterpret_cast<uint32_t*>(op) = E::pack(y, next);
+    part[threadIdx.x] = o;
+    __syncthreads();
+    if (g != 0) return;
+    for (int x = 1; x < groups; ++x) {
+        const float4 v = part[x * lanes + e];
+        o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+    }
+    T* op = (T*)out.data + (int64_t)b * out.stride + (int64_t)h * d + e * 4;
+    const float y0 = attended(l, o.x), y1 = attended(l, o.y), y2 = attended(l, o.z), y3 = attended(l, o.w);
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(op) = make_float4(y0, y1, y2, y3);
+    else *reinterpret_cast<uint2*>(op) = make_uint2(E::pack(y0, y1), E::pack(y2, y3));
 }
 
 }  // namespace
 
 int paged_splits(he_dtype dt, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len) {
     const int64_t groups = (int64_t)n_seqs * n_kv_heads;
-    const int64_t want = std::max<int64_t>(1, 4 * he_bf16::num_cus() / std::max<int64_t>(1, groups));
-    return (int)std::min<int64_t>(std::min<int64_t>(want, 64), std::max(1, (max_len + 127) / 128));
+    const int64_t want = std::max<int64_t>(1, 8 * he_bf16::num_cus() / std::max<int64_t>(1, groups));
+    return (int)std::min<int64_t>(std::min<int64_t>(want, kMostSplits), std::max(1, (max_len + 127) / 128));
 }
 
 void paged_attention(hipStream_t s, he_dtype dt, const Cache& c, Rows q, int n_heads, Rows out, const int32_t* lens, int n_seqs, int splits,
