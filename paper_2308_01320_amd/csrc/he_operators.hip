@@ -132,7 +132,7 @@ size_t he_paged_attention_workspace(const he_paged_cache* cache, int n_heads, in
     if (check_cache(cache, n_heads) || check_counts(n_seqs, 0)) return 0;
     if (n_seqs == 0) return 0;
     return split_bytes(n_seqs, n_heads, cache->head_dim,
-                       paged_splits(cache->dtype, n_heads, cache->n_kv_heads, cache->head_dim, n_seqs, longest_of(*cache, max_len)));
+                       paged_splits(cache->dtype, cache->page_size, n_heads, cache->n_kv_heads, n_seqs, longest_of(*cache, max_len)));
 }
 
 he_status he_paged_attention(const he_paged_cache* cache, const he_rows* q, int n_heads, const he_rows* out, const int32_t* d_lens, int n_seqs,
@@ -145,7 +145,7 @@ he_status he_paged_attention(const he_paged_cache* cache, const he_rows* q, int 
     if (!std::isfinite(scale)) return refuse(HE_ERR_INVALID_ARG, "scale is not finite");
     if (const he_status s = check_counts(n_seqs, 0)) return s;
     if (n_seqs == 0) return HE_OK;
-    const int splits = paged_splits(cache->dtype, n_heads, cache->n_kv_heads, cache->head_dim, n_seqs, longest_of(*cache, max_len));
+    const int splits = paged_splits(cache->dtype, cache->page_size, n_heads, cache->n_kv_heads, n_seqs, longest_of(*cache, max_len));
     const size_t need = split_bytes(n_seqs, n_heads, cache->head_dim, splits);
     if (need > workspace_bytes || (need && !d_workspace))
         return refuse(HE_ERR_CAPACITY, "workspace of %zu bytes, %zu are needed", d_workspace ? workspace_bytes : (size_t)0, need);

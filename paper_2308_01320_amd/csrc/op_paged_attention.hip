@@ -106,9 +106,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_mma_kernel(Cache
                                                                            float* __restrict__ workspace) {
     typedef typename E::T T;
     typedef PagedTile<E, DP, EXACT> Ti;
-    constexpr int KB = DP / 32, OB = DP / 16, PITCH = DP + 4, REGION = 2 * 32 * DP * 2;  // a wavefront's two tiles of V, in bytes
+    constexpr int WAVES = 4, KB = DP / 32, OB = DP / 16, PITCH = DP + 4, REGION = 2 * 32 * DP * 2;  // a wavefront's two tiles of V, in bytes
     extern __shared__ __align__(1024) unsigned char smem[];
-    __shared__ float2 ml[4][16];
+    __shared__ float2 ml[WAVES][16];
     const int d = EXACT ? DP : c.head_dim, share = n_heads / c.n_kv_heads, groups = (share + 15) / 16;
     const int part = blockIdx.x % splits, rest = blockIdx.x / splits, h = rest / groups, g0 = rest % groups * 16, b = blockIdx.y, nq = min(16, share - g0);
     const int len = (int)min((int64_t)max(lens[b], 0), (int64_t)c.pages_per_seq << c.page_shift);
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_mma_kernel(Cache
         }
     };
     u32x4 k[2][KB], qo[KB];
-    Pages now = pages(wave), next = pages(wave + 4);
+    Pages now = pages(wave), next = pages(wave + WAVES);
     if (wave < n_tiles) {
         request_v(now, wave, 0);
         asm volatile("" ::: "memory");  // K behind V: loads come back in order, so whoever has K has V in LDS
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_mma_kernel(Cache
     }
     float m = -INFINITY, l = 0.f;
     int buf = 0;
-    for (int tile = wave; tile < n_tiles; tile += 4) {
+    for (int tile = wave; tile < n_tiles; tile += WAVES) {
         f32x4 s[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -193,11 +193,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_mma_kernel(Cache
                 if (EXACT || kb * 32 < d) s[x] = mma16(E{}, k[x][kb], qo[kb], s[x]);
         }
         asm volatile("" : "+v"(s[0]), "+v"(s[1])::"memory");  // (K has been waited for, and with it V)
-        const Pages after = pages(tile + 8);
-        if (tile + 4 < n_tiles) {
-            request_v(next, tile + 4, buf ^ 1);  // (its reads were over when the tile before this one was)
+        const Pages after = pages(tile + 2 * WAVES);
+        if (tile + WAVES < n_tiles) {
+            request_v(next, tile + WAVES, buf ^ 1);  // (its reads were over when the tile before this one was)
             asm volatile("" ::: "memory");
-            request_k(next, tile + 4, k);
+            request_k(next, tile + WAVES, k);
         }
         const int t0 = begin + tile * 32;
         const int n0 = now.p[0] < 0 ? 0 : min(end - t0, 16), n1 = now.p[1] < 0 ? 0 : min(end - t0 - 16, 16);  // keys of each half
@@ -267,13 +267,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_mma_kernel(Cache
     if (g == 0) ml[wave][j] = make_float2(m, l);
     __syncthreads();
     const Partial part_at = partial_of(workspace, (size_t)gridDim.y * n_heads, splits);
-    for (int x = threadIdx.x; x < nq * (d / 2); x += 256) {
+    for (int x = threadIdx.x; x < nq * (d / 2); x += 64 * WAVES) {
         const int qi = x / (d / 2), e = x % (d / 2) * 2, head = h * share + g0 + qi;
         float top = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][qi].x);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[w][qi].x);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float2 a = ml[w][qi], v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(smem + w * REGION) + qi * PITCH + e);
             const float f = a.x > -INFINITY ? __builtin_amdgcn_exp2f(a.x - top) : a.y;
             sum += a.y * f;
@@ -336,10 +336,16 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ wor
 
 }  // namespace
 
-int paged_splits(he_dtype dt, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len) {
-    const int64_t groups = (int64_t)n_seqs * n_kv_heads;
-    const int64_t want = std::max<int64_t>(1, 8 * he_bf16::num_cus() / std::max<int64_t>(1, groups));
-    return (int)std::min<int64_t>(std::min<int64_t>(want, kMostSplits), std::max(1, (max_len + 127) / 128));
+// Splits of a sequence: enough workgroups for two to a CU (the vector units' kernel: four) as long as each has 128 positions, and up to eight to a CU
+// of 1024 positions and more, which even out sequences of different lengths.  us, with 2 / 4 / 8 to a CU: 4 sequences of up to 100003, 40/8 heads
+// 195.9 / 200.6 / 187.1; 32 of up to 511, 40/8 heads 17.0 / 19.1 / 19.1; 16 of up to 300, 32 heads of 64 9.7 / 12.7 / 13.0; float, 4 of up to 1000, 32 heads
+// 22.1 / 20.8 / 20.6.
+int paged_splits(he_dtype dt, int page_size, int n_heads, int n_kv_heads, int n_seqs, int max_len) {
+    const bool mma = dt != HE_F32 && page_size >= 16;
+    const int share = n_heads / n_kv_heads, per_group = mma ? 16 : 4;
+    const int64_t groups = (int64_t)n_seqs * n_kv_heads * ((share + per_group - 1) / per_group), cus = he_bf16::num_cus();
+    auto fill = [&](int to_a_cu, int positions) { return std::min<int64_t>((to_a_cu * cus + groups - 1) / groups, (max_len + positions - 1) / positions); };
+    return (int)std::min<int64_t>(std::max<int64_t>(std::max(fill(mma ? 2 : 4, 128), fill(8, 1024)), 1), kMostSplits);
 }
 
 void paged_attention(hipStream_t s, he_dtype dt, const Cache& c, Rows q, int n_heads, Rows out, const int32_t* lens, int n_seqs, int splits,
@@ -349,10 +355,11 @@ void paged_attention(hipStream_t s, he_dtype dt, const Cache& c, Rows q, int n_h
         typedef decltype(e) E;
         if constexpr (sizeof(typename E::T) == 2) {
             if (c.page_shift >= 4) {  // (a half of a tile lies in one page)
+                const int groups = c.n_kv_heads * ((share + 15) / 16) * splits;
                 auto launch = [&](auto dp, auto exact) {
                     constexpr int DP = decltype(dp)::value;
                     paged_mma_kernel<E, DP, decltype(exact)::value>
-                        <<<dim3(c.n_kv_heads * ((share + 15) / 16) * splits, n_seqs), 256, 4 * 2 * 32 * DP * 2, s>>>(c, q, n_heads, out, lens, splits, scale, workspace);
+                        <<<dim3(groups, n_seqs), 256, 4 * 2 * 32 * DP * 2, s>>>(c, q, n_heads, out, lens, splits, scale, workspace);
                 };
                 if (c.head_dim == 64) launch(std::integral_constant<int, 64>{}, std::true_type{});
                 else if (c.head_dim == 128) launch(std::integral_constant<int, 128>{}, std::true_type{});

@@ -106,7 +106,7 @@ struct Rope { int half, interleaved; double turns[128]; };  // half the rotated 
 void append(hipStream_t s, he_dtype dt, const Cache& c, const Rope& rope, Rows q, int n_heads, Rows q_out, Rows k, Rows k_out, Rows v,
             const int32_t* starts, const int32_t* lens, int n_seqs, int n_tokens);
 
-int paged_splits(he_dtype dt, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len);
+int paged_splits(he_dtype dt, int page_size, int n_heads, int n_kv_heads, int n_seqs, int max_len);
 void paged_attention(hipStream_t s, he_dtype dt, const Cache& c, Rows q, int n_heads, Rows out, const int32_t* lens, int n_seqs, int splits,
                      float scale, float* workspace);
 
