@@ -286,7 +286,7 @@ he_status he_score(he_engine* e, const int32_t* d_ids, int B, int T, float* d_ou
  * different streams and from different threads may overlap as long as they do not write the same memory.  Arguments are checked on the
  * host; what device memory holds (lengths, starts, page numbers) is bounds-checked by the kernels as stated.  head_dim is a multiple
  * of 16 up to 256, a row's head h lies h * head_dim elements behind the row's first, query heads h * n_heads / n_kv_heads and on
- * share key-value head h, and `data` pointers, rows and pages lie on 16 bytes.  Sums, soft-max statistics and rotations are float;
+ * share key-value head h, and `data` pointers, rows and pages lie on 16 bytes.  At most 65535 sequences, 2^23 rows, 65536 heads.  Sums, soft-max statistics and rotations are float;
  * results are rounded once to dtype. */
 
 /* Text of the last HE_ERR_ an operator gave the calling thread. */

@@ -19,7 +19,9 @@ __attribute__((format(printf, 2, 3))) he_status refuse(he_status s, const char* 
     return s;
 }
 
-constexpr int kMost = 1 << 30;  // rows, and positions of a sequence: indexes stay inside an int
+constexpr int kMost = 1 << 30;      // positions of a sequence: indexes stay inside an int
+constexpr int kMostRows = 1 << 23;  // rows of a packed batch: what a launch of a workgroup to each may have
+constexpr int64_t kMostGroups = (1 << 24) - 1;
 
 int elt_bytes(he_dtype t) { return t == HE_F32 ? 4 : 2; }
 bool known(he_dtype t) { return t == HE_F32 || t == HE_BF16 || t == HE_F16; }
@@ -69,7 +71,7 @@ Rows device_rows(const he_rows* r) { return r ? Rows{r->data, r->stride} : Rows{
 he_status check_counts(int n_seqs, int n_tokens) {
     if (n_seqs < 0 || n_tokens < 0) return refuse(HE_ERR_INVALID_ARG, "a negative number of sequences or rows");
     if (n_seqs > 65535) return refuse(HE_ERR_SHAPE, "%d sequences: 65535 at most", n_seqs);
-    if (n_tokens > kMost) return refuse(HE_ERR_SHAPE, "over 2^30 rows");
+    if (n_tokens > kMostRows) return refuse(HE_ERR_SHAPE, "%d rows: 2^23 at most", n_tokens);
     return HE_OK;
 }
 
@@ -146,6 +148,7 @@ he_status he_paged_attention(const he_paged_cache* cache, const he_rows* q, int 
     if (const he_status s = check_counts(n_seqs, 0)) return s;
     if (n_seqs == 0) return HE_OK;
     const int splits = paged_splits(cache->dtype, cache->page_size, n_heads, cache->n_kv_heads, n_seqs, longest_of(*cache, max_len));
+    if ((int64_t)n_seqs * n_heads > kMostGroups) return refuse(HE_ERR_SHAPE, "%d sequences of %d heads: 2^24 in all at most", n_seqs, n_heads);
     const size_t need = split_bytes(n_seqs, n_heads, cache->head_dim, splits);
     if (need > workspace_bytes || (need && !d_workspace))
         return refuse(HE_ERR_CAPACITY, "workspace of %zu bytes, %zu are needed", d_workspace ? workspace_bytes : (size_t)0, need);
@@ -167,6 +170,8 @@ he_status he_packed_attention(he_dtype dtype, const he_rows* q, int n_heads, con
     if (causal != 0 && causal != 1) return refuse(HE_ERR_INVALID_ARG, "causal must be 0 or 1");
     if (!std::isfinite(scale)) return refuse(HE_ERR_INVALID_ARG, "scale is not finite");
     if (const he_status s = check_counts(n_seqs, n_tokens)) return s;
+    if ((int64_t)(n_tokens / 32 + n_seqs) * n_heads > kMostGroups)
+        return refuse(HE_ERR_SHAPE, "%d rows, %d sequences, %d heads: (rows / 32 + sequences) heads is 2^24 at most", n_tokens, n_seqs, n_heads);
     if (n_seqs == 0 || n_tokens == 0) return HE_OK;
     packed_attention((hipStream_t)stream, dtype, device_rows(q), n_heads, device_rows(k), device_rows(v), n_kv_heads, head_dim, device_rows(out), d_seq_starts,
                      n_seqs, n_tokens, causal != 0, scale);

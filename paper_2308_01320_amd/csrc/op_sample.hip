@@ -717,8 +717,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Rows logits, int vocab
         if (rf.first_only) {
             lim.z = ask.topf;  // (more than fit of one value or little else: its first, below)
         } else {
-            if (whole_head && rate < 1e30) {  // (a temperature next to nothing: the rest's weights are no floats)
-                const bool complete = log_weight(cut, top, rate).zero;
+            if (whole_head && (rate < 1e30 || vocab <= kAllHead)) {  // (a temperature next to nothing: the rest's weights are no floats)
+                const bool complete = row.infinite || vocab <= kAllHead || log_weight(cut, top, rate).zero;
                 lim = limit_of(sh, head, ask, (unsigned long long)(rest * 4398046511104.0), complete, cut);
                 by_head = lim.all;
             }

@@ -72,7 +72,8 @@ def sample_row(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     V, top = len(z), z.max()
     if top == -np.inf:
         return -1, -np.inf
-    rel = np.where(z == top, 0.0, z - top)
+    with np.errstate(invalid="ignore"):
+        rel = np.where(z == top, 0.0, z - top)
     lse = np.log(np.exp(rel).sum())
     order = np.lexsort((np.arange(V), -z))
     if not temperature > 0:

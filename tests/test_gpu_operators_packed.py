@@ -132,3 +132,19 @@ def test_repeats_bit_for_bit_and_replays():
         assert torch.equal(out, want)
     starts.copy_(ints([0, 300, 301, 777]))
     assert torch.equal(B.he_packed_attention(q, k, v, starts), first)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [-0.3, 0.0])
+def test_scales_that_turn_or_level_the_scores(dtype, scale):
+    dt = R.DTYPES[dtype]
+    _, (q, k, v) = make(dt, 4, 2, 64, 90)
+    got = B.he_packed_attention(q.cuda(), k.cuda(), v.cuda(), ints([0, 70, 90]), scale=scale)
+    check(got.cpu(), q, k, v, [0, 70, 90], dt, True, scale)
+    pages = torch.randperm(12, generator=torch.Generator().manual_seed(1)).int().view(2, 6)
+    kp, vp = (torch.zeros(12, 2, 16, 64, dtype=dt).cuda() for _ in range(2))
+    B.he_paged_append(k.cuda(), v.cuda(), kp, vp, pages.cuda(), ints([0, 0]), seq_starts=ints([0, 70, 90]))
+    got = B.he_paged_attention(q[[69, 89]].cuda(), kp, vp, pages.cuda(), ints([70, 20]), scale=scale).cpu()
+    for i, (a, b) in enumerate(((0, 70), (70, 90))):
+        want, mag, most = R.attend(q[b - 1:b], k[a:b], v[a:b], scale)
+        R.check_attended(got[i:i + 1], want, mag, most, b - a, dt, 2.0 ** -16)

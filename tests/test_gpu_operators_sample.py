@@ -143,3 +143,30 @@ def test_replays_and_repeats():
         torch.cuda.synchronize()
         assert torch.equal(a, ids) and torch.equal(b, lp)
     check(z, u.cpu().tolist(), top_p=[float(np.float32(0.9))] * 16)
+
+
+@pytest.mark.parametrize("vocab", [1, 3, 5, 7, 9, 512, 513])
+def test_small_vocabularies(vocab):
+    """Fewer logits than a lane reads at a time, with every filter, infinities, and temperatures next to nothing."""
+    for dt in (torch.float32, torch.bfloat16):
+        z = logits(6, vocab, dt, 30 + vocab)
+        z[3, vocab // 2] = float("inf")
+        z[4, 1:] = -float("inf")
+        u = [0.1, 0.5, 0.9, 0.3, 0.7, 1.0]
+        check(z, u)
+        for t in (1.0, 1e-30, 1e-38):
+            check(z, u, temperature=[t] * 6, top_k=[2, 3, 4, 5, 6, 2], top_p=[0.9, 0.5, 0.99, 0.7, 0.3, 0.8], min_p=[0.0, 0.1, 0.01, 0.0, 0.0, 0.5])
+            check(z, u, temperature=[t] * 6, top_k=[2, 3, 4, 5, 6, 2])
+
+
+def test_deep_borders():
+    """Filters that keep far more of a row than its largest few thousand tokens, and rows whose largest tokens are many and equal."""
+    z = logits(8, 60000, torch.float32, 40, 1.0)
+    z[5, ::3] = 5.0
+    z[6, 1000:9000] = 7.5
+    z[7, :4096] = 3.25
+    u = [0.05, 0.3, 0.5, 0.7, 0.9, 0.2, 0.6, 0.99]
+    check(z, u, top_p=[0.99, 0.95, 0.9, 0.8, 0.999, 0.9, 0.97, 0.95], temperature=[1.3, 1.0, 2.0, 0.8, 1.0, 1.0, 0.7, 5.0])
+    check(z, u, top_k=[20000, 9000, 50000, 6000, 59999, 15000, 4000, 30000], top_p=[0.9, 0.99, 0.5, 0.7, 0.98, 0.6, 0.95, 0.9])
+    check(z, u, min_p=[0.01, 0.001, 1e-4, 0.05, 0.02, 0.5, 0.3, 0.1], top_p=[0.99] * 8, top_k=[30000] * 8)
+    check(z, u, temperature=[0.0] * 8)

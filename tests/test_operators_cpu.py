@@ -67,7 +67,7 @@ def test_append_refuses():
     assert append(seqs=-1) == append(n=-1) == 1
     assert append(starts=None, seqs=2, n=5) == 1
     assert b"5 rows, 2 sequences" in B.lib().he_operator_error()
-    assert append(seqs=65536, n=65536) == 2 and append(n=(1 << 30) + 1) == 2
+    assert append(seqs=65536, n=65536) == 2 and append(n=(1 << 23) + 1) == 2
     assert append(k=rows(P + 4)) == append(k=rows(stride=129)) == append(v=rows(stride=-8)) == 2
     assert append(k_out=rows(stride=120)) == 2  # rows that would overlap
     assert append(q=rows(), q_out=rows(), heads=3) == 2
@@ -92,6 +92,7 @@ def test_packed_attention_refuses():
     assert packed(dtype=3) == packed(causal=2) == packed(scale=float("nan")) == packed(seqs=-1) == packed(n=-1) == 1
     assert packed(heads=5) == packed(kv=0) == packed(d=40) == packed(d=512) == packed(q=rows(P + 8)) == packed(k=rows(stride=4)) == packed(out=rows(stride=128)) == 2
     assert packed(dtype=B.HE_F32, k=rows(stride=130)) == 2 and packed(seqs=65536) == 2
+    assert packed(n=1 << 23, heads=128, kv=2, q=rows(stride=8192), out=rows(stride=8192)) == 2  # (more workgroups than a launch may have)
     assert packed(seqs=0) == packed(n=0) == 0
 
 
