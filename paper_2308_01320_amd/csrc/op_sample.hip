@@ -12,6 +12,11 @@
 // log2 w names the step in which a filter's border lies, the tokens of that step are compared one with another, and the kept weights are
 // summed by spans of ids.  A row without filters needs one slice again, the one in which the number falls.  Else (flat rows) the same is done
 // over the whole row, with its own weights.
+//
+// What bounds it: 64-bit arithmetic (a weight is some 35 instructions, a third of them on doubles) and, in a row's one workgroup, the barriers and
+// passes one behind the other.  256 rows of 50272 bf16 logits, every filter: 22 us for the slices (26 MB), 42 for the rows; one row of floats 6 and 27,
+// or 77 where a top-p border lies deep in a flat row.  All of it in a row's workgroup, histogram and sums over the whole row: 88 and 104 us; a search for
+// the borders bit by bit: 2921 and 3073.
 #include <climits>
 
 #include "operators.h"
@@ -56,7 +61,7 @@ struct Shared {
     unsigned long long before_count, before_mass, last, kept_mass;
 };
 
-// (z - max) log2(e) / T + 42 in 1024ths: what of it is whole (`log`) and what is left of it, up to half a 1024th.  Zero: less than half a unit
+// (z - max) log2(e) / T + 42 in 1024ths: what of it is whole and what is left of it, up to half a 1024th.  Zero: less than half a unit
 // of weight, or nothing at all.
 struct Log { int whole; float rest; bool zero; };
 __device__ __forceinline__ Log log_weight(float z, double top, double rate) {
@@ -660,6 +665,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Rows logits, int vocab
             const double v = __shfl_up(upto, o);
             if (lane >= o) upto += v;
         }
+        __syncthreads();  // (everybody has the sums above)
         if (lane == 63) sh.wave_d[wave] = upto;
         if (threadIdx.x == 0) { sh.bin = -1; sh.list_n = -1; }
         __syncthreads();
