@@ -83,7 +83,7 @@ __device__ __forceinline__ int page_of(const Cache& c, int b, int t) {
 }
 // Where position t of key-value head h begins in page p, in elements from the start of K (or V)
 __device__ __forceinline__ size_t cache_row(const Cache& c, int p, int h, int t) {
-    return (size_t)p * c.page_stride + ((size_t)((h << c.page_shift) + (t & ((1 << c.page_shift) - 1)))) * c.head_dim;
+    return (size_t)p * c.page_stride + (((size_t)h << c.page_shift) + (t & ((1 << c.page_shift) - 1))) * c.head_dim;
 }
 
 // The sequence that packed row i belongs to: the last b of [0, n) with starts[b] <= i.  Sixty-four probes a step (one for each lane),
