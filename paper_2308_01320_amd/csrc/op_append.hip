@@ -15,7 +15,7 @@ namespace {
 // the two groups of eight that are each other's pairs, or eight pairs -- and goes over the heads of queries, keys and values 256 / (d/16)
 // apart, always with the same pairs, whose sines stay in registers.  Bound by memory: 8192 rows at most of 120 heads of 128 (321 MB) take 70 us, 4.6 TB/s
 // where a plain copy of 2 GiB reaches 5.1; a step of 32 rows of 56 heads 3.5 us in a graph, a launch and three dependent loads.  The values of the
-// first heads requested ahead of the position: 71 and 4.5 us, more registers and no less waiting.
+// first heads requested ahead of the position: 72.7 us for 70.8 and 7.0 for 5.0 (kernel times by themselves), more registers and no less waiting.
 template <class E>
 __global__ __launch_bounds__(256) void append_kernel(Cache c, Rope rope, Rows q, int n_heads, Rows q_out, Rows k, Rows k_out, Rows v,
                                                      const int32_t* __restrict__ starts, const int32_t* __restrict__ lens, int n_seqs) {
